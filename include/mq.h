@@ -23,7 +23,8 @@
  *     launch and nothing is enqueued when a call fails.  After a failure no
  *     output is defined.
  *   - Device pointers must be 16-byte aligned and all matrices are dense
- *     (row stride = row length) except W, which has `ldw`.
+ *     (row stride = row length) except W, which has `ldw`, and the X of
+ *     mq_quantize_tokens, which has `ldx`.
  *   - Reentrant: nothing is kept between calls that a result depends on.  Two
  *     calls may run concurrently, from one or several host threads, on different
  *     streams when their buffers (workspace included) do not overlap.
@@ -469,8 +470,89 @@ mq_status mq_linear_bwd_gated(const uint16_t *X, const uint8_t *Q, const float *
                               int64_t M, int64_t F, int64_t K, const int *rs, int nr, uint32_t flags,
                               uint16_t *dX, float *dW, void *ws, size_t ws_bytes, void *hip_stream);
 
+/*
+ * The layer in 8-bit integers.  The stored form of a weight is one code of at most 8 bits (section 3.1.1; sliced to r bits by
+ * section 3.2), so with the tokens quantized to 8 bits as well the product is one of whole numbers, which the matrix core forms at
+ * twice the bf16 rate without converting anything.  (The paper quantizes weights only; tokens in 8 bits, one scale each, are this
+ * library's choice.)  Serving only: a straight-through backward of the same layer is mq_linear_bwd.
+ *
+ * mq_quantize_tokens, for every token m:
+ *     scale_m = max_k |X[m,k]| / 127     Xq[m,k] = round(X[m,k] * (127 / max_k |X[m,k]|))     sum_m = sum_k Xq[m,k]
+ * fp32, one IEEE operation per symbol, round = half-to-even; codes -127 .. 127.  (A largest magnitude below 2^-100 and its row are
+ * multiplied by 2^100 first, so that the quotient stays finite.)  A row of zeros takes scale 0 and codes 0.  A row that holds an
+ * infinity or a NaN takes scale NaN and codes 0: every output of that token is then NaN, and no other token's is touched.
+ *   X      [M, ldx] bf16, ldx >= K a multiple of 8
+ *   Xq     [M, K] int8 out             scale [M] fp32 out, sum [M] int32 out
+ * K a multiple of 16, K <= 131072.  M == 0 is a no-op.
+ *
+ * mq_linear_fwd_int8:
+ *     Y[m,n] = bf16(scale_m * alpha_n * (2^(8-r) * sum_k Xq[m,k] codes[n,k] - z_n * sum_m))
+ * the sum over k exact in 32-bit integers (K <= 131072), the rest in fp32.  No order of summation shows in the result: a token's
+ * outputs are the same bits whatever the other sizes of the call are.
+ *   X      [M, K] bf16, quantized on the way as mq_quantize_tokens does (the two calls in sequence give the same bits)
+ *   codes  [N, K] uint8, the r-bit codes: for r = 8 the Q of mq_quantize_int8, for r < 8 the plane that mq_slice writes without
+ *          MQ_FLAG_PACKED (values 0 .. 2^r - 1; a value beyond 127 is read as negative there)
+ *   alpha, zero  [N] fp32 as mq_quantize_int8 wrote them          r  1..8
+ *   flags  0, or MQ_FLAG_GATED, with MQ_FLAG_FFN_SILU or without it: the layer is a stacked gate / up layer (channels 2 f and
+ *          2 f + 1 are a pair, as in mq_linear_fwd_multi_gated, N even) and Y [M, N / 2] receives
+ *          bf16(act(y_2f) * y_2f+1) of the fp32 outputs y, act = SiLU with MQ_FLAG_FFN_SILU, otherwise GELU in its tanh form.
+ *          Any other flag is refused (MQ_ERR_BITS)
+ *   Y      [M, N] bf16 out (with MQ_FLAG_GATED [M, N / 2]); may not overlap an input
+ *   ws     workspace of at least mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1)
+ * K a multiple of 16, K <= 131072; M and N are free below 2^31 - 256.  M == 0 or N == 0 is a no-op.
+ * mq_linear_fwd_int8_quantized: the same on tokens that mq_quantize_tokens has quantized (several layers on one input); no workspace.
+ */
+enum { MQ_FLAG_GATED = 128 };
+enum { MQ_OP_LINEAR_FWD_INT8 = 8, MQ_OP_EXPERTS_ROUTE = 9, MQ_OP_EXPERTS_FWD_INT8 = 10 };
+mq_status mq_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
+                             void *hip_stream);
+mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t N,
+                             int64_t K, int r, uint32_t flags, uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream);
+mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,
+                                       const float *alpha, const float *zero, int64_t M, int64_t N, int64_t K, int r, uint32_t flags,
+                                       uint16_t *Y, void *hip_stream);
+
+/*
+ * A feed-forward block whose weights are split over E experts, each a layer of its own in the form above (the feed-forward weights
+ * are what the paper quantizes, section 5; experts are stacked codes, so one mq_quantize_int8 call over [E * N, K] quantizes them
+ * all).  A router, the caller's, chooses `top` experts for every token and weighs them; then
+ *     mq_experts_route     groups the choices by expert,
+ *     mq_experts_fwd_int8  multiplies every group with its expert's codes (gate / up: rows = the tokens of the places; down: rows NULL),
+ *     mq_experts_combine   adds each token's outputs with their weights.
+ *
+ * mq_experts_route: the M * top choices, in the order of ids, sorted by expert (stable).
+ *   ids      [M, top] int32; an id outside 0 .. E-1 is no choice (padding, masked tokens)
+ *   offsets  [E + 1] int32 out: expert e has the places offsets[e] .. offsets[e+1]
+ *   rows     [M * top] int32 out: the token of a place; -1 from place offsets[E] on
+ *   place    [M, top] int32 out: the place of a choice, -1 where it is none
+ *   ws       workspace of at least mq_workspace_bytes(MQ_OP_EXPERTS_ROUTE, M * top, E, 0, 1); up to 4096 choices it may be NULL
+ * 1 <= E <= 1024, 1 <= top <= 1024, M * top below 2^31 - 256.  M == 0 writes offsets of zero.
+ *
+ * mq_experts_fwd_int8: for every place p of expert e
+ *     Y[p] = the layer of mq_linear_fwd_int8 with codes[e], alpha[e], zero[e] on token rows[p]
+ * with the same bits as that call.  Group sizes are read on the device; an expert without tokens costs nothing.
+ *   X        [M, K] bf16            rows [T] int32, values 0 .. M-1, or NULL: place p is token p (T <= M)
+ *   offsets  [E + 1] int32, ascending, offsets[E] <= T; rows of Y from offsets[E] on are not written.  (Values outside of that
+ *            give undefined outputs, but nothing outside the arrays is read or written.)
+ *   codes    [E, N, K] uint8        alpha, zero [E, N] fp32
+ *   Y        [T, N] bf16 out (with MQ_FLAG_GATED [T, N / 2])
+ *   ws       workspace of at least mq_workspace_bytes(MQ_OP_EXPERTS_FWD_INT8, max(M, T), N, K, 1)
+ * r, flags and limits as for mq_linear_fwd_int8, T below 2^31 - 256.  T == 0 or N == 0 is a no-op.
+ *
+ * mq_experts_combine:  out[m,n] = bf16(sum_j weight[m,j] * Y[place[m,j], n])   over the choices with 0 <= place[m,j] < T, in their
+ * order, in fp32; a token without any gets zeros.
+ *   Y [T, N] bf16;  place [M, top] int32;  weight [M, top] fp32;  out [M, N] bf16 out
+ */
+mq_status mq_experts_route(const int32_t *ids, int64_t M, int64_t top, int64_t E, int32_t *offsets, int32_t *rows, int32_t *place,
+                           void *ws, size_t ws_bytes, void *hip_stream);
+mq_status mq_experts_fwd_int8(const uint16_t *X, int64_t M, const int32_t *rows, const int32_t *offsets, const uint8_t *codes,
+                              const float *alpha, const float *zero, int64_t T, int64_t E, int64_t N, int64_t K, int r, uint32_t flags,
+                              uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream);
+mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place, const float *weight, int64_t T, int64_t M, int64_t top,
+                             int64_t N, uint16_t *out, void *hip_stream);
+
 /* Bytes of workspace for `op` at these sizes (0 on invalid arguments).  MQ_OP_FFN_DECODE: M = B, N = F, K = d.
- * MQ_OP_GEMV: M = B, nr = r (bits per code).
+ * MQ_OP_GEMV: M = B, nr = r (bits per code).  MQ_OP_EXPERTS_ROUTE: M = choices (tokens times top), N = E, K is not looked at.
  *
  * MQ_OP_LINEAR_FWD, MQ_OP_LINEAR_FWD_L2, MQ_OP_LINEAR_BWD, MQ_OP_LINEAR_BWD_CLIP: the bytes do not always grow with M.
  * Where few tokens would leave most of the GPU idle, contractions are cut into ranges whose fp32 partial sums (at most

@@ -27,15 +27,21 @@ MQ_OP_LINEAR_FWD_L2 = 4
 MQ_OP_LINEAR_BWD_CLIP = 5
 MQ_OP_AFFINE_BWD = 6
 MQ_OP_GEMV = 7
+MQ_OP_LINEAR_FWD_INT8 = 8
+MQ_OP_EXPERTS_ROUTE = 9
+MQ_OP_EXPERTS_FWD_INT8 = 10
 MQ_FLAG_LOSS_MIX = 64
 MQ_FLAG_FFN_SILU = 16
 MQ_FLAG_FFN_RESIDUAL = 32
+MQ_FLAG_GATED = 128
 
 EXPORTS = ["mq_quantize_int8", "mq_slice", "mq_linear_fwd_multi", "mq_linear_bwd", "mq_gemv_sliced",
            "mq_params_to_bf16", "mq_workspace_bytes", "mq_status_string",
            "mq_gemv_sliced_dense_ep", "mq_ffn_mixnmatch", "mq_matquant_l2_loss", "mq_linear_fwd_multi_l2", "mq_linear_bwd_clip",
            "mq_affine_weight", "mq_affine_input", "mq_affine_bwd", "mq_gated_unit_fwd", "mq_gated_unit_bwd",
-           "mq_linear_fwd_multi_noalloc", "mq_linear_bwd_gated", "mq_linear_fwd_multi_gated", "mq_slice_multi", "mq_gemv_sliced_ws"]
+           "mq_linear_fwd_multi_noalloc", "mq_linear_bwd_gated", "mq_linear_fwd_multi_gated", "mq_slice_multi", "mq_gemv_sliced_ws",
+           "mq_quantize_tokens", "mq_linear_fwd_int8", "mq_linear_fwd_int8_quantized", "mq_experts_route", "mq_experts_fwd_int8",
+           "mq_experts_combine"]
 
 
 class MqError(RuntimeError):
@@ -96,6 +102,12 @@ def _load() -> ctypes.CDLL:
     lib.mq_linear_bwd_clip.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, ctypes.POINTER(vp), ctypes.POINTER(ctypes.c_float),
                                        i64, i64, i64, ctypes.POINTER(ci), ci, u32, vp, vp, vp, vp, vp, sz, vp]
     lib.mq_ffn_mixnmatch.argtypes = [vp, ctypes.POINTER(_FfnLayer), ci, i64, i64, i64, u32, vp, vp, sz, vp]
+    lib.mq_quantize_tokens.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp]
+    lib.mq_linear_fwd_int8.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp, sz, vp]
+    lib.mq_linear_fwd_int8_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp]
+    lib.mq_experts_route.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.mq_experts_fwd_int8.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, u32, vp, vp, sz, vp]
+    lib.mq_experts_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp]
     for name in EXPORTS:
         if name not in ("mq_workspace_bytes", "mq_status_string"):
             getattr(lib, name).restype = ci
@@ -581,3 +593,122 @@ def mq_gated_unit_bwd(GU, dA, silu: bool = False, dGU=None):
     _check(st, "mq_gated_unit_bwd")
     return dGU
 
+
+def mq_quantize_tokens(X, Xq=None, scale=None, sums=None):
+    """Tokens X bf16 [M, K] (row stride allowed) -> (codes int8 [M, K], scale fp32 [M], sums of the codes int32 [M])."""
+    if X.dtype is not torch.bfloat16 or not X.is_cuda or X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError("X must be a 2-D bf16 GPU tensor with unit column stride")
+    M, K = X.shape
+    ldx = X.stride(0) if M > 1 else max(K, X.stride(0) & ~7)
+    Xq = torch.empty(M, K, dtype=torch.int8, device=X.device) if Xq is None else Xq
+    scale = torch.empty(M, dtype=torch.float32, device=X.device) if scale is None else scale
+    sums = torch.empty(M, dtype=torch.int32, device=X.device) if sums is None else sums
+    if Xq.shape != X.shape or scale.numel() != M or sums.numel() != M:
+        raise ValueError("outputs do not match X")
+    st = _lib.mq_quantize_tokens(X.data_ptr(), M, K, ldx, _ptr(Xq, torch.int8), _ptr(scale, torch.float32), _ptr(sums, torch.int32),
+                                 _stream())
+    _check(st, "mq_quantize_tokens")
+    return Xq, scale, sums
+
+
+_GATES = {None: 0, "gelu": MQ_FLAG_GATED, "silu": MQ_FLAG_GATED | MQ_FLAG_FFN_SILU}
+
+
+def _gate_flags(gate) -> int:
+    if gate not in _GATES:
+        raise ValueError("gate is None, 'gelu' or 'silu'")
+    return _GATES[gate]
+
+
+def mq_linear_fwd_int8(X, codes, alpha, zero, r: int, gate=None, Y=None, ws=None):
+    """The layer in 8-bit integers: X bf16 [M, K], codes uint8 [N, K] (the unpacked r-bit codes) -> Y bf16 [M, N], or with
+    gate "gelu" / "silu" (stacked gate / up channels) [M, N / 2]."""
+    M, K = X.shape
+    N = codes.shape[0]
+    n_out = N if gate is None else N // 2
+    if codes.shape[1] != K or alpha.numel() != N or zero.numel() != N:
+        raise ValueError("X, codes, alpha and zero disagree on N or K")
+    if Y is None:
+        Y = torch.empty(M, n_out, dtype=torch.bfloat16, device=X.device)
+    elif Y.shape != (M, n_out):
+        raise ValueError("Y has another shape")
+    if ws is None:
+        ws = torch.empty(max(mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1), 16), dtype=torch.uint8, device=X.device)
+    st = _lib.mq_linear_fwd_int8(_ptr(X, torch.bfloat16), _ptr(codes, torch.uint8), _ptr(alpha, torch.float32), _ptr(zero, torch.float32),
+                                 M, N, K, r, _gate_flags(gate), _ptr(Y, torch.bfloat16), _ptr(ws, torch.uint8), ws.numel(), _stream())
+    _check(st, "mq_linear_fwd_int8")
+    return Y
+
+
+def mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, r: int, gate=None, Y=None):
+    """mq_linear_fwd_int8 on the tokens that mq_quantize_tokens returned."""
+    M, K = Xq.shape
+    N = codes.shape[0]
+    n_out = N if gate is None else N // 2
+    if codes.shape[1] != K or alpha.numel() != N or zero.numel() != N or scale.numel() != M or sums.numel() != M:
+        raise ValueError("tokens, codes, alpha and zero disagree on M, N or K")
+    if Y is None:
+        Y = torch.empty(M, n_out, dtype=torch.bfloat16, device=Xq.device)
+    elif Y.shape != (M, n_out):
+        raise ValueError("Y has another shape")
+    st = _lib.mq_linear_fwd_int8_quantized(_ptr(Xq, torch.int8), _ptr(scale, torch.float32), _ptr(sums, torch.int32),
+                                           _ptr(codes, torch.uint8), _ptr(alpha, torch.float32), _ptr(zero, torch.float32), M, N, K, r,
+                                           _gate_flags(gate), _ptr(Y, torch.bfloat16), _stream())
+    _check(st, "mq_linear_fwd_int8_quantized")
+    return Y
+
+
+def mq_experts_route(ids, E: int, offsets=None, rows=None, place=None, ws=None):
+    """The choices ids int32 [M, top] grouped by expert: (offsets [E + 1], rows [M * top], place [M, top]), int32; an id outside
+    0 .. E-1 is no choice."""
+    M, top = ids.shape
+    offsets = torch.empty(E + 1, dtype=torch.int32, device=ids.device) if offsets is None else offsets
+    rows = torch.empty(M * top, dtype=torch.int32, device=ids.device) if rows is None else rows
+    place = torch.empty(M, top, dtype=torch.int32, device=ids.device) if place is None else place
+    if offsets.numel() != E + 1 or rows.numel() != M * top or place.shape != ids.shape:
+        raise ValueError("outputs do not match ids and E")
+    if ws is None:
+        ws = torch.empty(max(mq_workspace_bytes(MQ_OP_EXPERTS_ROUTE, M * top, E, 0, 1), 16), dtype=torch.uint8, device=ids.device)
+    st = _lib.mq_experts_route(_ptr(ids, torch.int32), M, top, E, _ptr(offsets, torch.int32), _ptr(rows, torch.int32),
+                               _ptr(place, torch.int32), _ptr(ws, torch.uint8), ws.numel(), _stream())
+    _check(st, "mq_experts_route")
+    return offsets, rows, place
+
+
+def mq_experts_fwd_int8(X, offsets, codes, alpha, zero, r: int, rows=None, gate=None, Y=None, ws=None):
+    """The layer in 8-bit integers by expert: X bf16 [M, K], codes uint8 [E, N, K], alpha, zero fp32 [E, N]; place p of expert e
+    (offsets[e] <= p < offsets[e + 1]) is token rows[p], or token p without rows -> Y bf16 [T, N], gated [T, N / 2]."""
+    M, K = X.shape
+    E, N, k = codes.shape
+    T = M if rows is None else rows.numel()
+    n_out = N if gate is None else N // 2
+    if k != K or alpha.numel() != E * N or zero.numel() != E * N or offsets.numel() != E + 1:
+        raise ValueError("X, offsets, codes, alpha and zero disagree on E, N or K")
+    if Y is None:
+        Y = torch.empty(T, n_out, dtype=torch.bfloat16, device=X.device)
+    elif Y.shape != (T, n_out):
+        raise ValueError("Y has another shape")
+    if ws is None:
+        ws = torch.empty(max(mq_workspace_bytes(MQ_OP_EXPERTS_FWD_INT8, max(M, T), N, K, 1), 16), dtype=torch.uint8, device=X.device)
+    st = _lib.mq_experts_fwd_int8(_ptr(X, torch.bfloat16), M, _ptr(rows, torch.int32), _ptr(offsets, torch.int32), _ptr(codes, torch.uint8),
+                                  _ptr(alpha, torch.float32), _ptr(zero, torch.float32), T, E, N, K, r, _gate_flags(gate),
+                                  _ptr(Y, torch.bfloat16), _ptr(ws, torch.uint8), ws.numel(), _stream())
+    _check(st, "mq_experts_fwd_int8")
+    return Y
+
+
+def mq_experts_combine(Y, place, weight, out=None):
+    """out[m] = sum over j of weight[m, j] Y[place[m, j]] (places of -1 left out): Y bf16 [T, N], place int32 and weight fp32
+    [M, top] -> bf16 [M, N]."""
+    M, top = place.shape
+    T, N = Y.shape
+    if weight.shape != place.shape:
+        raise ValueError("place and weight differ in shape")
+    if out is None:
+        out = torch.empty(M, N, dtype=torch.bfloat16, device=Y.device)
+    elif out.shape != (M, N):
+        raise ValueError("out has another shape")
+    st = _lib.mq_experts_combine(_ptr(Y, torch.bfloat16), _ptr(place, torch.int32), _ptr(weight, torch.float32), T, M, top, N,
+                                 _ptr(out, torch.bfloat16), _stream())
+    _check(st, "mq_experts_combine")
+    return out

@@ -1,0 +1,212 @@
+// Around the products by expert: the router's choices grouped by expert, and the weighted sum of the experts' outputs.
+#include "mq_int8.h"
+
+namespace mq {
+
+// ============================================================================================
+// grouping
+// ============================================================================================
+// A stable counting sort with E + 1 buckets, the last one for choices of no expert.  A workgroup takes kRouteChunk choices, a wave 64 of them
+// at a time.  Lanes with the same bucket find each other by comparing a bit of the bucket at a time; the first of them leaves their
+// number in count[64 choices][bucket], and sums over the earlier counts give every choice its place: no atomics, one order.
+constexpr int kRouteThreads = 1024, kRouteSteps = 4, kRouteChunk = kRouteThreads * kRouteSteps;
+
+struct RouteArgs {
+    const int32_t *ids;   // [n]
+    int32_t *offsets, *rows, *place;
+    int32_t *chunk_counts;  // [chunks][E + 1]
+    int n, top, E, chunks;
+};
+
+// PLACES false: only the counts of the chunk, into chunk_counts (launches of more than one chunk need them first).
+template <bool PLACES>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int buckets = a.E + 1, padded = (buckets + 1) & ~1;
+    constexpr int GROUPS = kRouteChunk / 64;
+    uint16_t *count = reinterpret_cast<uint16_t *>(smem);                        // [GROUPS][padded]
+    int32_t *base = reinterpret_cast<int32_t *>(smem + GROUPS * padded * 2);     // [padded] first place of this chunk's choices
+    int32_t *total = base + padded;                                              // [padded]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * kRouteChunk;
+
+    for (int i = threadIdx.x; i < GROUPS * padded / 2; i += kRouteThreads) reinterpret_cast<uint32_t *>(smem)[i] = 0;
+    __syncthreads();
+    int bucket[kRouteSteps], rank[kRouteSteps];
+#pragma unroll
+    for (int s = 0; s < kRouteSteps; ++s) {
+        const int i = first + s * kRouteThreads + (int)threadIdx.x;
+        bucket[s] = -1;   // past the end: a bucket of its own that nobody counts
+        if (i < a.n) {
+            const int id = a.ids[i];
+            bucket[s] = id >= 0 && id < a.E ? id : a.E;
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < kRouteSteps; ++s) {
+        uint64_t same = __ballot(bucket[s] >= 0);
+        for (int bit = 0; (1 << bit) < buckets; ++bit) {
+            const bool set = bucket[s] >> bit & 1;
+            const uint64_t with = __ballot(set);
+            same &= set ? with : ~with;
+        }
+        rank[s] = __popcll(same & ((1ull << lane) - 1));
+        if (bucket[s] >= 0 && rank[s] == 0) count[(s * (kRouteThreads / 64) + wave) * padded + bucket[s]] = (uint16_t)__popcll(same);
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < buckets; b += kRouteThreads) {
+        int sum = 0;
+        for (int g = 0; g < GROUPS; ++g) {
+            const int c = count[g * padded + b];
+            count[g * padded + b] = (uint16_t)sum;
+            sum += c;
+        }
+        if constexpr (PLACES) {
+            int before = 0, all = sum;
+            if (a.chunks > 1) {
+                all = 0;
+                for (int c = 0; c < a.chunks; ++c) {
+                    const int v = a.chunk_counts[(int64_t)c * buckets + b];
+                    before += c < (int)blockIdx.x ? v : 0;
+                    all += v;
+                }
+            }
+            base[b] = before;
+            total[b] = all;
+        } else {
+            a.chunk_counts[(int64_t)blockIdx.x * buckets + b] = sum;
+        }
+    }
+    if constexpr (PLACES) {
+        __syncthreads();
+        if (wave == 0) {  // prefix sums of the totals, 64 buckets at a time
+            int carry = 0;
+            for (int b0 = 0; b0 < buckets; b0 += 64) {
+                const int b = b0 + lane, mine = b < buckets ? total[b] : 0;
+                int upto = mine;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int v = __shfl_up(upto, o, 64);
+                    if (lane >= o) upto += v;
+                }
+                if (b < buckets) {
+                    base[b] += carry + upto - mine;
+                    if (blockIdx.x == 0) a.offsets[b] = carry + upto - mine;
+                }
+                carry += __shfl(upto, 63, 64);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kRouteSteps; ++s) {
+            if (bucket[s] < 0) continue;
+            const int i = first + s * kRouteThreads + (int)threadIdx.x;
+            const int p = base[bucket[s]] + count[(s * (kRouteThreads / 64) + wave) * padded + bucket[s]] + rank[s];
+            a.rows[p] = bucket[s] < a.E ? i / a.top : -1;
+            a.place[i] = bucket[s] < a.E ? p : -1;
+        }
+    }
+}
+
+// ============================================================================================
+// weighted sum
+// ============================================================================================
+struct CombineArgs {
+    const uint16_t *Y;
+    const int32_t *place;
+    const float *weight;
+    uint16_t *out;
+    int64_t M, N;
+    int top, T;
+};
+
+template <int V>  // values per thread: 8 where rows are whole 16-byte chunks, otherwise 1
+__global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
+    const int64_t chunks = a.N / V, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.M * chunks) return;
+    const int64_t m = i / chunks, n = (i - m * chunks) * V;
+    float sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.f;
+    for (int j = 0; j < a.top; ++j) {
+        const int p = a.place[m * a.top + j];
+        if (p < 0 || p >= a.T) continue;
+        const float w = a.weight[m * a.top + j];
+        const uint16_t *y = a.Y + (int64_t)p * a.N + n;
+        if constexpr (V == 8) {
+            const u32x4 d = *reinterpret_cast<const u32x4 *>(y);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                sum[2 * v] = __builtin_fmaf(w, bf16_lo(d[v]), sum[2 * v]);
+                sum[2 * v + 1] = __builtin_fmaf(w, bf16_hi(d[v]), sum[2 * v + 1]);
+            }
+        } else {
+            sum[0] = __builtin_fmaf(w, bf16_bits_to_float(*y), sum[0]);
+        }
+    }
+    uint16_t *out = a.out + m * a.N + n;
+    if constexpr (V == 8)
+        *reinterpret_cast<u32x4 *>(out) = u32x4{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]), pack_bf16x2(sum[4], sum[5]),
+                                                pack_bf16x2(sum[6], sum[7])};
+    else
+        *out = (uint16_t)float_to_bf16_bits(sum[0]);
+}
+
+namespace {
+
+int route_lds(int64_t E) {
+    const int padded = (int)((E + 2) & ~(int64_t)1);
+    return kRouteChunk / 64 * padded * 2 + 2 * padded * 4;
+}
+
+template <bool PLACES>
+mq_status launch_route(const RouteArgs &a, hipStream_t st) {
+    const int lds = route_lds(a.E);
+    if (!allow_lds<route_kernel<PLACES>>(lds)) return MQ_ERR_DEVICE;
+    route_kernel<PLACES><<<dim3((unsigned)a.chunks), dim3(kRouteThreads), lds, st>>>(a);
+    return launch_status();
+}
+
+}  // namespace
+
+size_t route_workspace_bytes(int64_t n, int64_t E) {
+    if (E < 1 || E > kMaxExperts || n > 0x7FFFFF00) return 0;
+    return (size_t)cdiv(n, kRouteChunk) * (size_t)(E + 1) * 4 + 256;
+}
+
+}  // namespace mq
+
+extern "C" mq_status mq_experts_route(const int32_t *ids, int64_t M, int64_t top, int64_t E, int32_t *offsets, int32_t *rows, int32_t *place,
+                                      void *ws, size_t ws_bytes, void *hip_stream) {
+    using namespace mq;
+    if (M < 0 || top < 1 || E < 1 || E > kMaxExperts || top > kMaxExperts || M > 0x7FFFFF00 / top) return MQ_ERR_SHAPE;
+    if (!offsets || (M > 0 && (!ids || !rows || !place))) return MQ_ERR_NULL;
+    if (!aligned16(ids) || !aligned16(offsets) || !aligned16(rows) || !aligned16(place)) return MQ_ERR_ALIGN;
+    RouteArgs a{ids, offsets, rows, place, nullptr, (int)(M * top), (int)top, (int)E, (int)(M == 0 ? 1 : cdiv(M * top, kRouteChunk))};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (a.chunks > 1) {
+        if (!ws || !aligned16(ws) || ws_bytes < route_workspace_bytes(a.n, E)) return MQ_ERR_WORKSPACE;
+        a.chunk_counts = reinterpret_cast<int32_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+        const mq_status s = launch_route<false>(a, st);
+        if (s != MQ_OK) return s;
+    }
+    return launch_route<true>(a, st);
+}
+
+extern "C" mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place, const float *weight, int64_t T, int64_t M, int64_t top,
+                                        int64_t N, uint16_t *out, void *hip_stream) {
+    using namespace mq;
+    if (M < 0 || N < 0 || T < 0 || top < 1 || top > kMaxExperts || M > 0x7FFFFF00 || N > 0x7FFFFF00 || T > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    if (M == 0 || N == 0) return MQ_OK;
+    if ((T > 0 && !Y) || !place || !weight || !out) return MQ_ERR_NULL;
+    if (!aligned16(Y) || !aligned16(place) || !aligned16(weight) || !aligned16(out)) return MQ_ERR_ALIGN;
+    const CombineArgs a{Y, place, weight, out, M, N, (int)top, (int)T};
+    const int V = N % 8 == 0 ? 8 : 1;
+    const int64_t blocks = cdiv(M * (N / V), 256);
+    if (blocks > 0x7FFFFFFF) return MQ_ERR_SHAPE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (V == 8)
+        combine_kernel<8><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
+    else
+        combine_kernel<1><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
+    return launch_status();
+}

@@ -1,0 +1,224 @@
+// The layer in 8-bit integers: tokens quantized to int8 with a scale each, times the codes of the weights as they are stored, on the
+// matrix core's 8-bit product (twice the rate of the bf16 one, and nothing is converted).  Quantizer of tokens, entry points.
+#include "mq_int8.h"
+
+namespace mq {
+
+// ============================================================================================
+// quantizer of tokens
+// ============================================================================================
+// scale = top / 127, code = round(x (127 / top)) with top the row's largest magnitude, sum = the row's codes added up.  One read of the
+// row into registers, so 2 bytes read and 1 written per value; the largest magnitude is found on the bf16 bits themselves (their order is
+// that of the magnitudes, infinities and NaN last).
+// TPR threads to a row, V chunks of 8 values in each.
+template <int TPR, int V, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *__restrict__ X, int64_t M, int K, int64_t ldx,
+                                                                int8_t *__restrict__ Xq, float *__restrict__ scale,
+                                                                int32_t *__restrict__ sum) {
+    constexpr int WAVES = TPR / 64;  // to a row
+    __shared__ uint32_t tops[BLOCK / 64];
+    __shared__ int32_t sums[BLOCK / 64];
+    const int t = threadIdx.x % TPR, wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
+    const int64_t m = (int64_t)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
+    const bool live = m < M;
+    const u32x4 *src = reinterpret_cast<const u32x4 *>(X + (live ? m : 0) * ldx);
+    u32x4 v[V];
+    uint32_t top2 = 0;  // largest magnitude of the low and of the high halves
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        v[i] = u32x4{0u, 0u, 0u, 0u};
+        const int c = t + i * TPR;
+        if (live && c * 8 < K) v[i] = src[c];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            top2 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top2),
+                                                                          __builtin_bit_cast(u16x2, v[i][w] & 0x7FFF7FFFu)));
+    uint32_t top = max(top2 & 0xFFFFu, top2 >> 16);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = max(top, tops[first + w]);
+    }
+    const bool finite = top < 0x7F80u;
+    const float most = bf16_bits_to_float(top);
+    const float lift = most < 0x1p-100f ? 0x1p100f : 1.0f;          // 127 / most would pass the largest fp32 number
+    const float per = finite && top != 0 ? __fdiv_rn(127.0f, most * lift) : 0.0f;
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int c = t + i * TPR;
+        uint32_t out[2] = {0u, 0u};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t d = finite ? v[i][w] : 0u;  // (infinity times zero is no number)
+            const int lo = (int)rintf(bf16_lo(d) * lift * per), hi = (int)rintf(bf16_hi(d) * lift * per);
+            total += lo + hi;
+            out[w >> 1] |= ((uint32_t)(lo & 0xFF) | (uint32_t)(hi & 0xFF) << 8) << (16 * (w & 1));
+        }
+        if (live && c * 8 < K) *reinterpret_cast<u32x2 *>(Xq + m * K + c * 8) = u32x2{out[0], out[1]};
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) sums[wave] = total;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) total += sums[first + w];
+    }
+    if (live && t == 0) {
+        scale[m] = finite ? __fdiv_rn(most, 127.0f) : __uint_as_float(0x7FC00000u);
+        sum[m] = total;
+    }
+}
+
+namespace {
+
+template <int TPR, int V, int BLOCK>
+mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum, hipStream_t st) {
+    quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(M, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(X, M, (int)K, ldx, Xq, scale, sum);
+    return launch_status();
+}
+
+// ---- workspace of the calls that take bf16 tokens -------------------------------------------------------------
+struct Int8Layout {
+    size_t codes, scale, sum, total;
+};
+Int8Layout int8_layout(int64_t M, int64_t K) {
+    Int8Layout l;
+    size_t off = 0;
+    l.codes = off, off += align256((size_t)M * K);
+    l.scale = off, off += align256((size_t)M * 4);
+    l.sum = off, off += align256((size_t)M * 4);
+    l.total = off + 256;
+    return l;
+}
+
+// sizes, bits and flags of a product
+mq_status check_int8(int64_t M, int64_t N, int64_t K, int r, uint32_t flags) {
+    if (M < 0 || N < 0 || K < 1 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > kInt8MaxK) return MQ_ERR_SHAPE;
+    if (r < 1 || r > 8) return MQ_ERR_BITS;
+    if (flags & ~(uint32_t)(MQ_FLAG_GATED | MQ_FLAG_FFN_SILU)) return MQ_ERR_BITS;
+    if (K % 16 != 0 || ((flags & MQ_FLAG_GATED) && N % 2 != 0)) return MQ_ERR_ALIGN;
+    return MQ_OK;
+}
+
+mq_status check_weights(const uint8_t *codes, const float *alpha, const float *zero, const uint16_t *Y) {
+    if (!codes || !alpha || !zero || !Y) return MQ_ERR_NULL;
+    if (!aligned16(codes) || !aligned16(alpha) || !aligned16(zero) || !aligned16(Y)) return MQ_ERR_ALIGN;
+    return MQ_OK;
+}
+
+Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t T, int64_t N, int64_t K, int64_t E, int r,
+                   uint32_t flags, uint16_t *Y) {
+    Int8Args a{};
+    a.codes = codes;
+    a.alpha = alpha;
+    a.zero = zero;
+    a.Y = Y;
+    a.M = (int)M;
+    a.T = (int)T;
+    a.N = (int)N;
+    a.K = (int)K;
+    a.E = (int)E;
+    a.gate = !(flags & MQ_FLAG_GATED) ? 0 : (flags & MQ_FLAG_FFN_SILU) ? 2 : 1;
+    a.mult = (float)(1 << (8 - r));
+    a.offset = r == 8 ? 128.0f : 0.0f;
+    return a;
+}
+
+// quantizes the tokens into the workspace and multiplies them
+mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t ws_bytes, hipStream_t st) {
+    const Int8Layout l = int8_layout(a.M, a.K);
+    if (!ws || !aligned16(ws) || ws_bytes < l.total) return MQ_ERR_WORKSPACE;
+    uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+    int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
+    float *scale = reinterpret_cast<float *>(base + l.scale);
+    int32_t *sum = reinterpret_cast<int32_t *>(base + l.sum);
+    const mq_status s = launch_quantize_tokens(X, a.M, a.K, a.K, Xq, scale, sum, st);
+    if (s != MQ_OK) return s;
+    a.Xq = Xq;
+    a.scale = scale;
+    a.sum = sum;
+    return launch_int8_blocks(a, st);
+}
+
+}  // namespace
+
+mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
+                                 hipStream_t st) {
+    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
+    if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
+    return launch_tokens<1024, 16, 1024>(X, M, K, ldx, Xq, scale, sum, st);
+}
+
+size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    (void)N;
+    return K < 1 || K > kInt8MaxK ? 0 : int8_layout(M, K).total;
+}
+
+}  // namespace mq
+
+extern "C" mq_status mq_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
+                                        void *hip_stream) {
+    using namespace mq;
+    if (M < 0 || K < 1 || M > 0x7FFFFF00 || K > kInt8MaxK || ldx < K || ldx > ((int64_t)1 << 40)) return MQ_ERR_SHAPE;
+    if (K % 16 != 0 || ldx % 8 != 0) return MQ_ERR_ALIGN;
+    if (M == 0) return MQ_OK;
+    if (!X || !Xq || !scale || !sum) return MQ_ERR_NULL;
+    if (!aligned16(X) || !aligned16(Xq) || !aligned16(scale) || !aligned16(sum)) return MQ_ERR_ALIGN;
+    return launch_quantize_tokens(X, M, K, ldx, Xq, scale, sum, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,
+                                                  const float *alpha, const float *zero, int64_t M, int64_t N, int64_t K, int r,
+                                                  uint32_t flags, uint16_t *Y, void *hip_stream) {
+    using namespace mq;
+    mq_status s = check_int8(M, N, K, r, flags);
+    if (s != MQ_OK || M == 0 || N == 0) return s;
+    if (!Xq || !scale || !sum) return MQ_ERR_NULL;
+    s = check_weights(codes, alpha, zero, Y);
+    if (s != MQ_OK) return s;
+    if (!aligned16(Xq) || !aligned16(scale) || !aligned16(sum)) return MQ_ERR_ALIGN;
+    Int8Args a = int8_args(codes, alpha, zero, M, M, N, K, 1, r, flags, Y);
+    a.Xq = Xq;
+    a.scale = scale;
+    a.sum = sum;
+    return launch_int8_blocks(a, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t N,
+                                        int64_t K, int r, uint32_t flags, uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream) {
+    using namespace mq;
+    mq_status s = check_int8(M, N, K, r, flags);
+    if (s != MQ_OK || M == 0 || N == 0) return s;
+    if (!X) return MQ_ERR_NULL;
+    s = check_weights(codes, alpha, zero, Y);
+    if (s != MQ_OK) return s;
+    if (!aligned16(X)) return MQ_ERR_ALIGN;
+    return quantize_and_multiply(int8_args(codes, alpha, zero, M, M, N, K, 1, r, flags, Y), X, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" mq_status mq_experts_fwd_int8(const uint16_t *X, int64_t M, const int32_t *rows, const int32_t *offsets, const uint8_t *codes,
+                                         const float *alpha, const float *zero, int64_t T, int64_t E, int64_t N, int64_t K, int r,
+                                         uint32_t flags, uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream) {
+    using namespace mq;
+    mq_status s = check_int8(M, N, K, r, flags);
+    if (s != MQ_OK) return s;
+    if (T < 0 || T > 0x7FFFFF00 || E < 1 || E > kMaxExperts || (!rows && T > M) || (T > 0 && M == 0)) return MQ_ERR_SHAPE;
+    if (T == 0 || N == 0) return MQ_OK;
+    if (!X || !offsets) return MQ_ERR_NULL;
+    s = check_weights(codes, alpha, zero, Y);
+    if (s != MQ_OK) return s;
+    if (!aligned16(X) || !aligned16(offsets) || (rows && !aligned16(rows))) return MQ_ERR_ALIGN;
+    Int8Args a = int8_args(codes, alpha, zero, M, T, N, K, E, r, flags, Y);
+    a.rows = rows;
+    a.offsets = offsets;
+    return quantize_and_multiply(a, X, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+}
