@@ -92,5 +92,7 @@ __device__ __forceinline__ int token_of(const Int8Args &a, int place) { return a
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
                                  hipStream_t st);
 mq_status launch_int8_blocks(const Int8Args &a, hipStream_t st);
+mq_status launch_int8_tiles(const Int8Args &a, hipStream_t st);
+mq_status launch_int8(const Int8Args &a, hipStream_t st);
 
 }  // namespace mq

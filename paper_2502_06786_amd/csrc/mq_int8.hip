@@ -146,7 +146,7 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
-    return launch_int8_blocks(a, st);
+    return launch_int8(a, st);
 }
 
 }  // namespace
@@ -156,6 +156,10 @@ mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_
     if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
     if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
     return launch_tokens<1024, 16, 1024>(X, M, K, ldx, Xq, scale, sum, st);
+}
+
+mq_status launch_int8(const Int8Args &a, hipStream_t st) {
+    return a.T / a.E >= 96 ? launch_int8_tiles(a, st) : launch_int8_blocks(a, st);
 }
 
 size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
@@ -190,7 +194,7 @@ extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float 
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
-    return launch_int8_blocks(a, static_cast<hipStream_t>(hip_stream));
+    return launch_int8(a, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t N,
