@@ -38,16 +38,26 @@ __device__ __forceinline__ i32x4 mfma_i8(const i32x4 &a, const i32x4 &b, const i
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-// scale alpha (2^(8-r) dot - (zero - offset) sum): the same fp32 steps in every kernel, and `dot` is a sum of whole numbers, so the
+// scale (alpha 2^(8-r) dot - alpha (zero - offset) sum): the same fp32 steps in every kernel, and `dot` is a sum of whole numbers, so the
 // outputs of all forms of the product are the same bits.  (dot and sum below 2^31 are rounded to fp32: 2^-24 of terms that the
-// centring keeps to the size of the result.)  alpha first: scale may be as small as a bf16 subnormal / 127.
-__device__ __forceinline__ float int8_output(int dot, float sum, float scale, float alpha, float zero, float mult, float offset) {
-    const float t = (zero - offset) * sum;
-    return (alpha * __builtin_fmaf(mult, (float)dot, -t)) * scale;
+// centring keeps near the size of the result.)  The token's scale last: it may be as small as a bf16 subnormal / 127.
+__device__ __forceinline__ void channel_factors(const f32x4 &alpha, const f32x4 &zero, float mult, float offset, f32x4 &ka, f32x4 &kb) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        ka[e] = alpha[e] * mult;
+        kb[e] = alpha[e] * (zero[e] - offset);
+    }
+}
+__device__ __forceinline__ float int8_output(int dot, float sum, float scale, float ka, float kb) {
+    return __builtin_fmaf(ka, (float)dot, -(kb * sum)) * scale;
 }
 
-// (the gate acts on the fp32 outputs: one rounding, to bf16, at the end)
-__device__ __forceinline__ float gated_value(float g, float u, int gate) { return (gate == 2 ? silu(g) : gelu_tanh(g)) * u; }
+// act(g) u, act(v) = v / (1 + exp(-t)): t = v for SiLU, 2 sqrt(2 / pi) (v + 0.044715 v^3) for GELU in its tanh form.  The gate acts on
+// the fp32 outputs: one rounding, to bf16, at the end.  (The reciprocal is the hardware's, 2^-23 of its value off at most.)
+__device__ __forceinline__ float gated_value(float g, float u, int gate) {
+    const float t = gate == 2 ? g : 1.5957691216057308f * (g + 0.044715f * g * g * g);
+    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-t)) * u;
+}
 
 // The `block`-th block of BM places, counted expert by expert: no block holds places of two experts.
 struct Block {
@@ -89,8 +99,8 @@ inline int64_t block_bound(int64_t T, int64_t E, bool grouped, int BM) { return 
 // the token of a place (rows are data: whatever they hold, tokens stay below M)
 __device__ __forceinline__ int token_of(const Int8Args &a, int place) { return a.rows ? min(max(a.rows[place], 0), a.M - 1) : place; }
 
-mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
-                                 hipStream_t st);
+mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
+                                 float *scale, int32_t *sum, hipStream_t st);
 mq_status launch_int8_blocks(const Int8Args &a, hipStream_t st);
 mq_status launch_int8_tiles(const Int8Args &a, hipStream_t st);
 mq_status launch_int8(const Int8Args &a, hipStream_t st);

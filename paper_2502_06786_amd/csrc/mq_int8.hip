@@ -11,9 +11,10 @@ namespace mq {
 // row into registers, so 2 bytes read and 1 written per value; the largest magnitude is found on the bf16 bits themselves (their order is
 // that of the magnitudes, infinities and NaN last).
 // TPR threads to a row, V chunks of 8 values in each.
+// rows: null, or the row of X that row m of the result is made of (rows are data: whatever they hold, they stay below X_rows).
 template <int TPR, int V, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *__restrict__ X, int64_t M, int K, int64_t ldx,
-                                                                int8_t *__restrict__ Xq, float *__restrict__ scale,
+                                                                const int32_t *__restrict__ rows, int X_rows, int8_t *__restrict__ Xq, float *__restrict__ scale,
                                                                 int32_t *__restrict__ sum) {
     constexpr int WAVES = TPR / 64;  // to a row
     __shared__ uint32_t tops[BLOCK / 64];
@@ -21,7 +22,9 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
     const int t = threadIdx.x % TPR, wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
     const int64_t m = (int64_t)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
     const bool live = m < M;
-    const u32x4 *src = reinterpret_cast<const u32x4 *>(X + (live ? m : 0) * ldx);
+    int64_t from = live ? m : 0;
+    if (rows) from = min(max(rows[from], 0), X_rows - 1);
+    const u32x4 *src = reinterpret_cast<const u32x4 *>(X + from * ldx);
     u32x4 v[V];
     uint32_t top2 = 0;  // largest magnitude of the low and of the high halves
 #pragma unroll
@@ -81,8 +84,9 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
 namespace {
 
 template <int TPR, int V, int BLOCK>
-mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum, hipStream_t st) {
-    quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(M, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(X, M, (int)K, ldx, Xq, scale, sum);
+mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, float *scale,
+                        int32_t *sum, hipStream_t st) {
+    quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(M, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(X, M, (int)K, ldx, rows, (int)X_rows, Xq, scale, sum);
     return launch_status();
 }
 
@@ -135,14 +139,20 @@ Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, 
 
 // quantizes the tokens into the workspace and multiplies them
 mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t ws_bytes, hipStream_t st) {
-    const Int8Layout l = int8_layout(a.M, a.K);
+    const Int8Layout l = int8_layout(a.M > a.T ? a.M : a.T, a.K);
     if (!ws || !aligned16(ws) || ws_bytes < l.total) return MQ_ERR_WORKSPACE;
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
     int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
     float *scale = reinterpret_cast<float *>(base + l.scale);
     int32_t *sum = reinterpret_cast<int32_t *>(base + l.sum);
-    const mq_status s = launch_quantize_tokens(X, a.M, a.K, a.K, Xq, scale, sum, st);
+    // gathered tokens past 2 GiB are quantized in the order of the places: the kernels address those that they gather with 32 bits
+    const bool placed = a.rows && (int64_t)a.M * a.K > 0x7FFFFFFF;
+    const mq_status s = launch_quantize_tokens(X, placed ? a.T : a.M, a.K, a.K, placed ? a.rows : nullptr, a.M, Xq, scale, sum, st);
     if (s != MQ_OK) return s;
+    if (placed) {
+        a.rows = nullptr;
+        a.M = a.T;
+    }
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
@@ -151,11 +161,11 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
 
 }  // namespace
 
-mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, int8_t *Xq, float *scale, int32_t *sum,
-                                 hipStream_t st) {
-    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
-    if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, Xq, scale, sum, st);
-    return launch_tokens<1024, 16, 1024>(X, M, K, ldx, Xq, scale, sum, st);
+mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
+                                 float *scale, int32_t *sum, hipStream_t st) {
+    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
+    if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
+    return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
 }
 
 mq_status launch_int8(const Int8Args &a, hipStream_t st) {
@@ -177,7 +187,7 @@ extern "C" mq_status mq_quantize_tokens(const uint16_t *X, int64_t M, int64_t K,
     if (M == 0) return MQ_OK;
     if (!X || !Xq || !scale || !sum) return MQ_ERR_NULL;
     if (!aligned16(X) || !aligned16(Xq) || !aligned16(scale) || !aligned16(sum)) return MQ_ERR_ALIGN;
-    return launch_quantize_tokens(X, M, K, ldx, Xq, scale, sum, static_cast<hipStream_t>(hip_stream));
+    return launch_quantize_tokens(X, M, K, ldx, nullptr, M, Xq, scale, sum, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,

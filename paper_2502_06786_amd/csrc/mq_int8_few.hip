@@ -29,11 +29,15 @@ __global__ __launch_bounds__(256) void int8_block_kernel(Int8Args a, int tiles_n
     const float s = a.scale[m], sum = (float)a.sum[m];
     const float *alpha = a.alpha + (int64_t)b.expert * a.N, *zero = a.zero + (int64_t)b.expert * a.N;
     float y[4];
+    f32x4 al, ze, ka, kb;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int n = n0 + 4 * g4 + e;
-        y[e] = n < a.N ? int8_output(acc[e], sum, s, alpha[n], zero[n], a.mult, a.offset) : 0.f;
+        al[e] = alpha[min(n0 + 4 * g4 + e, a.N - 1)];
+        ze[e] = zero[min(n0 + 4 * g4 + e, a.N - 1)];
     }
+    channel_factors(al, ze, a.mult, a.offset, ka, kb);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[e], sum, s, ka[e], kb[e]);
     const int n = n0 + 4 * g4;
     if (a.gate) {
         uint16_t *out = a.Y + (int64_t)place * (a.N / 2) + n / 2;

@@ -4,170 +4,243 @@
 
 namespace mq {
 
-// 16 zero bytes: what stands past the end of a token's row
-__device__ u32x4 int8_zeros = {0u, 0u, 0u, 0u};
-
-// In place in the accumulator file.  The compiler does not see a matrix product here (see mfma16_acc for why and for the waits that
-// are ours then): an operand that a vector instruction has written is used two wait states later at the earliest, an accumulator
-// read eight after its product.
+// In place.  The compiler does not see a matrix product here (see mfma16_acc for why and for the waits that are ours then): an operand
+// that a vector instruction has written is used two wait states later at the earliest, an accumulator read eight after its product.
 __device__ __forceinline__ void mfma_i8_acc(i32x4 &acc, const i32x4 &a, const i32x4 &b) {
-    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b));
 }
 
-// Four waves, WR x WC of them, each with RB blocks of 16 channels times TB blocks of 16 places; stages of 64 k, NBUF of them in LDS.
-template <int RB, int TB, int WR, int WC, int NBUF>
+// A value that the compiler takes for new: what depends on it is formed here and not kept in registers from before a loop.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// WR x WC waves, each with RB blocks of 16 channels times TB blocks of 16 places; stages of 128 k, two of them in LDS; then the scale,
+// zero-point, token scale and token sum of the tile's rows for two tiles, and for each wave 16 rows of outputs.
+template <int RB, int TB, int WR, int WC>
 struct Int8Tile {
-    static constexpr int TN = 16 * RB * WR, TM = 16 * TB * WC;
-    static constexpr int STAGE = (TN + TM) * 64;
-    static constexpr int OS = TN * 2 + 16;   // bytes of a row of the staged outputs
-    static constexpr int LDS = NBUF * STAGE > TM * OS ? NBUF * STAGE : TM * OS;
+    static constexpr int NW = WR * WC, TN = 16 * RB * WR, TM = 16 * TB * WC;
+    static constexpr int STAGE = (TN + TM) * 128;
+    static constexpr int PARAMS = 2 * STAGE, PARAM_SET = (TN + TM) * 8;
+    static constexpr int OUT = PARAMS + 2 * PARAM_SET, OS = RB * 32 + 16;   // OS: bytes of a row of outputs
+    static constexpr int LDS = OUT + NW * 16 * OS;
 };
 
-template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS>
-__global__ __launch_bounds__(256, WGS) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n) {
+// Persistent: workgroup i takes tiles i, i + gridDim.x, ...; the first stages of a tile are requested before the outputs of the one
+// before are formed.
+template <bool R8, int RB, int TB, int WR, int WC, int WGS>
+__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
-    constexpr int CL = T::TN / 64, XL = T::TM / 64, LPS = CL + XL, NM = RB * TB;
-    static_assert(WR * WC == 4 && T::TN % 64 == 0 && T::TM % 64 == 0, "");
+    typedef Int8Tile<RB, TB, WR, WC> T;
+    typedef __attribute__((address_space(1))) void *global_ptr;
+    constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL, NM = RB * TB;
+    static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0 && T::TN % 64 == 0 && T::TM % 64 == 0 && T::LDS <= 160 * 1024, "");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g4 = lane >> 4, l16 = lane & 15, wr = wave / WC, wc = wave % WC;
+    const int total = tiles_m * tiles_n;
 
-    const uint32_t lid = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    constexpr int GROUP = 4;
-    const int width = GROUP * tiles_n;
-    const int first_m = (int)(lid / width) * GROUP;
-    const int gsz = min(tiles_m - first_m, GROUP);
-    const Block b = find_block(a, first_m + (int)(lid % width) % gsz, T::TM);
-    if (b.count <= 0) return;
-    const int n0 = (int)(lid % width) / gsz * T::TN;
-
-    const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
-    uint32_t coff;
-    int col;
-    u8_tile_lane<4>(wave, lane, 0, (uint32_t)a.K, coff, col);
-    const uint32_t cstep = 64u * (uint32_t)a.K;
-    const int8_t *xrow[XL];
-#pragma unroll
-    for (int i = 0; i < XL; ++i) {
-        const int row = wave * 16 + (lane >> 2) + 64 * i;
-        xrow[i] = a.Xq + (int64_t)token_of(a, b.place + min(row, b.count - 1)) * a.K + col;
-    }
-
-    // load i of stage kt; past the end of the rows zeros, so that every stage has as many loads in flight
-    auto issue_one = [&](int kt, int i) {
-        const int k0 = kt * 64;
-        uint8_t *to = smem + kt % NBUF * T::STAGE + (wave + (i < CL ? i : i - CL) * 4) * 1024;
-        if (i < CL) {
-            const uint32_t off = k0 + col < a.K ? coff + (uint32_t)k0 : kOOB;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rC, (lds_ptr)to, 16, off + (uint32_t)i * cstep, 0, 0, 0);
-        } else {
-            const void *from = k0 + col < a.K ? (const void *)(xrow[i - CL] + k0) : (const void *)&int8_zeros;
-            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)from, (lds_ptr)(to + T::TN * 64), 16, 0, 0);
-        }
+    struct Tile {
+        Block b;
+        int n0;
+    };
+    auto tile_at = [&](int id) {
+        const uint32_t lid = xcd_contiguous_id(id, total);
+        constexpr int GROUP = 4;
+        const int width = GROUP * tiles_n;
+        const int first_m = (int)(lid / width) * GROUP;
+        const int gsz = min(tiles_m - first_m, GROUP);
+        return Tile{find_block(a, first_m + (int)(lid % width) % gsz, T::TM), (int)(lid % width) / gsz * T::TN};
     };
 
-    const int sw = (group_chunk(g4) ^ ((l16 >> 2) & 3)) << 4;
-    const uint32_t ca = (wr * 16 * RB + l16) * 64 + sw, xa = T::TN * 64 + (wc * 16 * TB + l16) * 64 + sw;  // + 1024 per block of 16
+    uint32_t coff[CL];
+    int col;
+    bf16_tile_lane<NW>(wave, lane, 0, (uint32_t)a.K, coff[0], col);   // (rows of eight 16-byte chunks as there)
+    col *= 2;
+#pragma unroll
+    for (int i = 1; i < CL; ++i) coff[i] = coff[0] + (uint32_t)(8 * NW * i) * (uint32_t)a.K;
+    __amdgpu_buffer_rsrc_t rC, rX;
+    uint32_t xoff[XL];
 
-    i32x4 acc[RB][TB];
+    // Load i of the stage at k0 into buffer `buf`.  INSIDE: the stage lies within the rows; otherwise what stands past their end is
+    // requested out of range, which the buffer unit answers with zeros, so that every stage has as many loads in flight.
+    auto issue_one = [&](auto inside_tag, int k0, int buf, int i) {
+        constexpr bool INSIDE = decltype(inside_tag)::value;
+        uint8_t *to = smem + buf * T::STAGE + (wave + i * NW) * 1024;   // (the rows of the tokens follow those of the codes)
+        const uint32_t off = i < CL ? coff[i] : xoff[i - CL];
+        if constexpr (INSIDE)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, off, k0, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, k0 + col < a.K ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
+    };
+    // A tile's parameters (set `set`) and its first two stages.
+    auto begin = [&](const Tile &t, int set) {
+        const int lane = here(threadIdx.x & 63);
+        rC = make_rsrc(a.codes + ((int64_t)t.b.expert * a.N + t.n0) * a.K, (uint64_t)(a.N - t.n0) * a.K);
+        const int64_t base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: launch_int8)
+        rX = make_rsrc(a.Xq + base * a.K, (uint64_t)(a.M - base) * a.K);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+        for (int i = 0; i < XL; ++i) {
+            const int row = wave * 8 + (lane >> 3) + 8 * NW * i;
+            xoff[i] = (uint32_t)(token_of(a, t.b.place + min(row, t.b.count - 1)) - (int)base) * (uint32_t)a.K + (uint32_t)col;
+        }
+        uint8_t *to = smem + T::PARAMS + set * T::PARAM_SET;
+        for (int i = wave; i < (T::TN + T::TM) / 64; i += NW) {   // 64 rows at a time
+            const bool channels = i < T::TN / 64;
+            const int row = (channels ? i : i - T::TN / 64) * 64 + lane;
+            const void *one, *two;
+            if (channels) {
+                const int64_t n = (int64_t)t.b.expert * a.N + min(t.n0 + row, a.N - 1);
+                one = a.alpha + n, two = a.zero + n;
+            } else {
+                const int m = token_of(a, t.b.place + min(row, t.b.count - 1));
+                one = a.scale + m, two = a.sum + m;
+            }
+            __builtin_amdgcn_global_load_lds((global_ptr)one, (lds_ptr)(to + i * 512), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)two, (lds_ptr)(to + i * 512 + 256), 4, 0, 0);
+        }
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < LPS; ++i) issue_one(std::false_type{}, s * 128, s, i);
+    };
 
+    // operands of half t of a stage; + 2048 per block of 16 rows
+    uint32_t ca[2], xa[2];
 #pragma unroll
-    for (int s = 0; s < NBUF; ++s)
-#pragma unroll
-        for (int i = 0; i < LPS; ++i) issue_one(s, i);
-    stage_barrier<(NBUF - 1) * LPS, 0>();
+    for (int t = 0; t < 2; ++t) {
+        const int sw = ((2 * group_chunk(g4) + t) ^ ((l16 >> 1) & 7)) << 4;
+        ca[t] = (wr * 16 * RB + l16) * 128 + sw;
+        xa[t] = T::TN * 128 + (wc * 16 * TB + l16) * 128 + sw;
+    }
+    i32x4 acc[RB][TB], wf[2][RB], xf[TB];   // wf: for the two halves of a stage
 
-    i32x4 wf[2][RB], xf[TB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca + rb * 1024));
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa + tb * 1024);
-
-    auto stage = [&](auto set_tag, int kt) {
-        constexpr int S = decltype(set_tag)::value;
-        // stage kt + 1 has landed, every wave has read stage kt; stages kt + 2 .. may be on their way
-        stage_barrier<(NBUF - 2) * LPS, 0>();
-        const uint8_t *nxt = smem + (kt + 1) % NBUF * T::STAGE;
+    // Half t of the stage at k0, which lies in buffer buf: blocks of places one after the other, the operands of a block replaced by those
+    // of the next half after its last product.  Half 0 reads the operands of half 1; then the buffer is free, and the loads of the stage
+    // after the next go there while half 1 reads the first operands of the next stage.  (The workgroup meets a few products after the
+    // last of these reads, not right behind it.)
+    auto half = [&](auto inside_tag, auto t_tag, int k0, int buf) {
+        constexpr int t = decltype(t_tag)::value;
+        const uint8_t *src = smem + (t == 0 ? buf : 1 - buf) * T::STAGE;
         static_for<NM>([&](auto q_tag) {
             constexpr int q = decltype(q_tag)::value, tb = q / RB, rb = q % RB;
-            mfma_i8_acc(acc[rb][tb], wf[S][rb], xf[tb]);
+            mfma_i8_acc(acc[rb][tb], wf[t][rb], xf[tb]);
+            if constexpr (t == 1 && q == RB - 1) stage_barrier<0, 0>();   // the next stage has landed, every wave has read this one
+            if constexpr (rb == RB - 1) xf[tb] = *reinterpret_cast<const i32x4 *>(src + xa[1 - t] + tb * 2048);
             static_for<RB>([&](auto j_tag) {
                 constexpr int j = decltype(j_tag)::value;
-                if constexpr (q == j * (NM / (4 * RB) > 1 ? NM / (4 * RB) : 1)) wf[1 - S][j] = *reinterpret_cast<const i32x4 *>(nxt + ca + j * 1024);
-                if constexpr (R8 && q == NM / 2 + j * (NM / 2 - 3) / RB) {
-                    wf[1 - S][j] = signed_codes<R8>(wf[1 - S][j]);
-                    asm volatile("" : "+v"(wf[1 - S][j]));   // here and not where it is used
+                if constexpr (q == RB + j * (NM / 2 - RB) / RB) wf[1 - t][j] = *reinterpret_cast<const i32x4 *>(src + ca[1 - t] + j * 2048);
+                if constexpr (R8 && q == NM / 2 + 2 + j * (NM / 2 - 5) / RB) {
+                    wf[1 - t][j] = signed_codes<R8>(wf[1 - t][j]);
+                    asm volatile("" : "+v"(wf[1 - t][j]));   // here and not where it is used
                 }
             });
-            if constexpr (rb == RB - 1) xf[tb] = *reinterpret_cast<const i32x4 *>(nxt + xa + tb * 1024);
-            static_for<LPS>([&](auto l_tag) {
+            static_for<t == 1 ? LPS : 0>([&](auto l_tag) {
                 constexpr int l = decltype(l_tag)::value;
-                if constexpr (q == NM / 4 + l * (NM / 2) / LPS) issue_one(kt + NBUF, l);
+                if constexpr (q == RB + 1 + l * (NM / 2) / LPS) issue_one(inside_tag, k0 + 256, buf, l);
             });
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    const int nkt = (a.K + 63) / 64;
-    for (int kt = 0; kt < nkt; kt += 2) {   // (after an odd number of stages one of zeros)
-        stage(std::integral_constant<int, 0>{}, kt);
-        stage(std::integral_constant<int, 1>{}, kt + 1);
-    }
-    mfma16_settle();
-    wait_vm0();  // (loads past the end must not land in the staged outputs)
-    __syncthreads();
 
-    // ---- outputs: staged as rows of bf16, stored as whole rows -------------------------------------------
-    const float *alpha = a.alpha + (int64_t)b.expert * a.N, *zero = a.zero + (int64_t)b.expert * a.N;
-    float sc[TB], sm[TB];
+    // the outputs of a tile, 16 places at a time through LDS that only this wave uses
+    auto finish = [&](auto gated_tag, const Tile &t, int set) {
+        constexpr bool GATED = decltype(gated_tag)::value;
+        const int lane = here(threadIdx.x & 63), g4 = lane >> 4, l16 = lane & 15;
+        const uint8_t *params = smem + T::PARAMS + set * T::PARAM_SET;
+        uint8_t *out = smem + T::OUT + wave * 16 * T::OS;
+        constexpr int shift = GATED ? 1 : 0;
+        const int n_out = a.N >> shift, first = (t.n0 + wr * 16 * RB) >> shift;
+        f32x4 ka[RB], kb[RB];
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
-        const int m = token_of(a, b.place + min(wc * 16 * TB + tb * 16 + l16, b.count - 1));
-        sc[tb] = a.scale[m];
-        sm[tb] = (float)a.sum[m];
-    }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const int nloc = (wr * RB + rb) * 16 + 4 * g4;
-        float al[4], ze[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int n = min(n0 + nloc + e, a.N - 1);
-            al[e] = alpha[n];
-            ze[e] = zero[n];
+        for (int rb = 0; rb < RB; ++rb) {
+            const int n = (wr * RB + rb) * 16 + 4 * g4;
+            const uint8_t *at = params + (n >> 6) * 512 + (n & 63) * 4;
+            channel_factors(*reinterpret_cast<const f32x4 *>(at), *reinterpret_cast<const f32x4 *>(at + 256), a.mult, a.offset, ka[rb], kb[rb]);
         }
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
-            float y[4];
+            const int row0 = (wc * TB + tb) * 16;
+            if (row0 >= t.b.count) break;
+            const uint8_t *at = params + T::TN * 8 + ((row0 + l16) >> 6) * 512 + ((row0 + l16) & 63) * 4;
+            const float scale = *reinterpret_cast<const float *>(at), sum = (float)*reinterpret_cast<const int32_t *>(at + 256);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sm[tb], sc[tb], al[e], ze[e], a.mult, a.offset);
-            uint8_t *to = smem + (wc * 16 * TB + tb * 16 + l16) * T::OS;
+            for (int rb = 0; rb < RB; ++rb) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum, scale, ka[rb][e], kb[rb][e]);
+                if constexpr (GATED)
+                    *reinterpret_cast<uint32_t *>(out + l16 * T::OS + rb * 16 + 4 * g4) =
+                        pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
+                else
+                    *reinterpret_cast<u32x2 *>(out + l16 * T::OS + rb * 32 + 8 * g4) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            constexpr int per = (2 * RB) >> shift;   // chunks of 8 outputs in a row
+            const int rows = min(16, t.b.count - row0);
+            uint16_t *y = a.Y + (int64_t)(t.b.place + row0) * n_out + first;
+            if (n_out % 8 == 0) {
+#pragma unroll
+                for (int i = 0; i < (16 * per + 63) / 64; ++i) {
+                    const int c = i * 64 + lane, row = c / per, ch = c % per;
+                    if (row < rows && first + ch * 8 < n_out)
+                        __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(out + row * T::OS + ch * 16),
+                                                    reinterpret_cast<u32x4 *>(y + (int64_t)row * n_out + ch * 8));
+                }
+            } else {
+                for (int c = lane; c < rows * per * 8; c += 64) {
+                    const int row = c / (per * 8), ch = c % (per * 8);
+                    if (first + ch < n_out) y[(int64_t)row * n_out + ch] = *reinterpret_cast<const uint16_t *>(out + row * T::OS + ch * 2);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+
+    int id = blockIdx.x, set = 0;
+    Tile cur = tile_at(id);
+    if (cur.b.count > 0) begin(cur, set);
+    for (;;) {
+        const int next_id = id + (int)gridDim.x;
+        Tile next = {};
+        if (next_id < total) next = tile_at(next_id);
+        if (cur.b.count > 0) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
+            stage_barrier<LPS, 0>();
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca[0] + rb * 2048));
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa[0] + tb * 2048);
+            int k0 = 0, buf = 0;
+            auto stage = [&](auto inside_tag) {
+                half(inside_tag, std::integral_constant<int, 0>{}, k0, buf);
+                half(inside_tag, std::integral_constant<int, 1>{}, k0, buf);
+                k0 += 128;
+                buf = 1 - buf;
+            };
+            while (k0 + 384 <= a.K) stage(std::true_type{});
+            while (k0 < a.K) stage(std::false_type{});
+            mfma16_settle();
+            stage_barrier<0, 0>();   // the buffers are free
+        }
+        if (next.b.count > 0) begin(next, 1 - set);
+        if (cur.b.count > 0) {
             if (a.gate)
-                *reinterpret_cast<uint32_t *>(to + nloc) = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
+                finish(std::true_type{}, cur, set);
             else
-                *reinterpret_cast<u32x2 *>(to + nloc * 2) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+                finish(std::false_type{}, cur, set);
         }
-    }
-    __syncthreads();
-    const int shift = a.gate ? 1 : 0, cols = T::TN >> shift, first = n0 >> shift, n_out = a.N >> shift;
-    if (n_out % 8 == 0) {
-        const int per = cols / 8;
-        for (int c = threadIdx.x; c < b.count * per; c += 256) {
-            const int row = c / per, ch = c % per;
-            if (first + ch * 8 < n_out)
-                __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(smem + row * T::OS + ch * 16),
-                                            reinterpret_cast<u32x4 *>(a.Y + (int64_t)(b.place + row) * n_out + first + ch * 8));
-        }
-    } else {
-        for (int c = threadIdx.x; c < b.count * cols; c += 256) {
-            const int row = c / cols, ch = c % cols;
-            if (first + ch < n_out) a.Y[(int64_t)(b.place + row) * n_out + first + ch] = *reinterpret_cast<const uint16_t *>(smem + row * T::OS + ch * 2);
-        }
+        if (next_id >= total) break;
+        id = next_id;
+        cur = next;
+        set = 1 - set;
     }
 #else
     (void)a;
@@ -176,21 +249,22 @@ __global__ __launch_bounds__(256, WGS) void int8_tile_kernel(Int8Args a, int til
 
 namespace {
 
-template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS>
+template <bool R8, int RB, int TB, int WR, int WC, int WGS>
 mq_status launch_tile(const Int8Args &a, hipStream_t st) {
-    typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
+    typedef Int8Tile<RB, TB, WR, WC> T;
     const int64_t tiles_n = cdiv(a.N, T::TN), tiles_m = block_bound(a.T, a.E, a.offsets != nullptr, T::TM);
-    if (tiles_n * tiles_m > 0x7FFFFFFF) return MQ_ERR_SHAPE;
-    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, NBUF, WGS>;
+    if (tiles_n * tiles_m > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, WGS>;
     if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;
-    kernel<<<dim3((unsigned)(tiles_n * tiles_m)), dim3(256), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n);
+    const int64_t most = 256 * WGS;   // workgroups that fit the GPU
+    kernel<<<dim3((unsigned)(tiles_n * tiles_m < most ? tiles_n * tiles_m : most)), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n);
     return launch_status();
 }
 
 }  // namespace
 
 #ifndef MQ_TILE
-#define MQ_TILE 8, 8, 2, 2, 4, 1
+#define MQ_TILE 4, 8, 4, 2, 1
 #endif
 mq_status launch_int8_tiles(const Int8Args &a, hipStream_t st) {
     return a.offset != 0.f ? launch_tile<true, MQ_TILE>(a, st) : launch_tile<false, MQ_TILE>(a, st);
