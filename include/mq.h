@@ -500,7 +500,10 @@ mq_status mq_linear_bwd_gated(const uint16_t *X, const uint8_t *Q, const float *
  *   Y      [M, N] bf16 out (with MQ_FLAG_GATED [M, N / 2]); may not overlap an input
  *   ws     workspace of at least mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1)
  * K a multiple of 16, K <= 131072; M and N are free below 2^31 - 256.  M == 0 or N == 0 is a no-op.
- * mq_linear_fwd_int8_quantized: the same on tokens that mq_quantize_tokens has quantized (several layers on one input); no workspace.
+ * With few tokens K may be cut into ranges whose partial sums (64 MiB at most) go through the workspace.  One that holds the tokens
+ * but not these (made for other sizes of the layer) is accepted: K is then not cut, which is slower; the results' bits are the same.
+ * mq_linear_fwd_int8_quantized: the same on tokens that mq_quantize_tokens has quantized (several layers on one input).  ws may be
+ * NULL: K is then not cut.
  */
 enum { MQ_FLAG_GATED = 128 };
 enum { MQ_OP_LINEAR_FWD_INT8 = 8, MQ_OP_EXPERTS_ROUTE = 9, MQ_OP_EXPERTS_FWD_INT8 = 10 };
@@ -510,7 +513,7 @@ mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const floa
                              int64_t K, int r, uint32_t flags, uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream);
 mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,
                                        const float *alpha, const float *zero, int64_t M, int64_t N, int64_t K, int r, uint32_t flags,
-                                       uint16_t *Y, void *hip_stream);
+                                       uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
  * A feed-forward block whose weights are split over E experts, each a layer of its own in the form above (the feed-forward weights

@@ -104,7 +104,7 @@ def _load() -> ctypes.CDLL:
     lib.mq_ffn_mixnmatch.argtypes = [vp, ctypes.POINTER(_FfnLayer), ci, i64, i64, i64, u32, vp, vp, sz, vp]
     lib.mq_quantize_tokens.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp]
     lib.mq_linear_fwd_int8.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp, sz, vp]
-    lib.mq_linear_fwd_int8_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp]
+    lib.mq_linear_fwd_int8_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp, sz, vp]
     lib.mq_experts_route.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.mq_experts_fwd_int8.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, u32, vp, vp, sz, vp]
     lib.mq_experts_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp]
@@ -640,7 +640,7 @@ def mq_linear_fwd_int8(X, codes, alpha, zero, r: int, gate=None, Y=None, ws=None
     return Y
 
 
-def mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, r: int, gate=None, Y=None):
+def mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, r: int, gate=None, Y=None, ws=None):
     """mq_linear_fwd_int8 on the tokens that mq_quantize_tokens returned."""
     M, K = Xq.shape
     N = codes.shape[0]
@@ -651,9 +651,11 @@ def mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, r: int, ga
         Y = torch.empty(M, n_out, dtype=torch.bfloat16, device=Xq.device)
     elif Y.shape != (M, n_out):
         raise ValueError("Y has another shape")
+    if ws is None:
+        ws = torch.empty(max(mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1), 16), dtype=torch.uint8, device=Xq.device)
     st = _lib.mq_linear_fwd_int8_quantized(_ptr(Xq, torch.int8), _ptr(scale, torch.float32), _ptr(sums, torch.int32),
                                            _ptr(codes, torch.uint8), _ptr(alpha, torch.float32), _ptr(zero, torch.float32), M, N, K, r,
-                                           _gate_flags(gate), _ptr(Y, torch.bfloat16), _stream())
+                                           _gate_flags(gate), _ptr(Y, torch.bfloat16), _ptr(ws, torch.uint8), ws.numel(), _stream())
     _check(st, "mq_linear_fwd_int8_quantized")
     return Y
 

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libmq.so")
 PROBE_DIR = os.path.join(HERE, "bench_probes")
 PROBE_LIB = os.path.join(PROBE_DIR, "libmq_probe.so")
 SOURCES = ["mq_quantize.hip", "mq_slice.hip", "mq_gemv.hip", "mq_gemv_quad.hip", "mq_gemv_ovf.hip", "mq_gemv_reg.hip", "mq_linear.hip", "mq_linear_split.hip", "mq_linear_wide.hip", "mq_ffn.hip", "mq_loss.hip", "mq_clip.hip", "mq_affine.hip",
-           "mq_int8.hip", "mq_int8_few.hip", "mq_int8_tile.hip", "mq_experts.hip"]
+           "mq_int8.hip", "mq_int8_few.hip", "mq_int8_mid.hip", "mq_int8_tile.hip", "mq_experts.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -87,7 +87,7 @@ size_t clip_workspace_bytes(int64_t M, int64_t N, int64_t K, int nr);
 // workspace of mq_affine_bwd (mq_affine.hip)
 size_t affine_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // workspace of mq_linear_fwd_int8 and mq_experts_fwd_int8 (mq_int8.hip)
-size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K, bool grouped);
 // workspace of mq_experts_route for n choices (mq_experts.hip)
 size_t route_workspace_bytes(int64_t n, int64_t E);
 // G[i] [N, K] = lambda_i dY_i^T X for nr gradients against one X (mq_linear.hip).  dw_each_bytes: the workspace it can use, or

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "mq_gemv.h"
+#include "mq_int8_plan.h"
 
 namespace mq {
 
@@ -101,8 +102,10 @@ __device__ __forceinline__ int token_of(const Int8Args &a, int place) { return a
 
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
                                  float *scale, int32_t *sum, hipStream_t st);
-mq_status launch_int8_blocks(const Int8Args &a, hipStream_t st);
-mq_status launch_int8_tiles(const Int8Args &a, hipStream_t st);
-mq_status launch_int8(const Int8Args &a, hipStream_t st);
+mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
+// places: of a tile, 32 or 64; part: room for the partial sums of `splits` ranges of K
+mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st);
+// places: of a tile, 128 or 256
+mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st);
 
 }  // namespace mq

@@ -1,5 +1,7 @@
 // The layer in 8-bit integers: tokens quantized to int8 with a scale each, times the codes of the weights as they are stored, on the
 // matrix core's 8-bit product (twice the rate of the bf16 one, and nothing is converted).  Quantizer of tokens, entry points.
+#include <algorithm>
+
 #include "mq_int8.h"
 
 namespace mq {
@@ -90,9 +92,9 @@ mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, co
     return launch_status();
 }
 
-// ---- workspace of the calls that take bf16 tokens -------------------------------------------------------------
+// ---- workspace: the quantized tokens, then the partial sums of ranges of K, if there are any ---------------------------
 struct Int8Layout {
-    size_t codes, scale, sum, total;
+    size_t codes, scale, sum, part;
 };
 Int8Layout int8_layout(int64_t M, int64_t K) {
     Int8Layout l;
@@ -100,8 +102,23 @@ Int8Layout int8_layout(int64_t M, int64_t K) {
     l.codes = off, off += align256((size_t)M * K);
     l.scale = off, off += align256((size_t)M * 4);
     l.sum = off, off += align256((size_t)M * 4);
-    l.total = off + 256;
+    l.part = off;
     return l;
+}
+Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64_t part_bytes) {
+    return remembered<Int8Plan>(make_int8_plan, T, N, K, E, std::min(part_bytes, kInt8PartBytes));
+}
+
+// `part`: room of part_bytes for partial sums, 256-byte aligned
+mq_status launch_int8(const Int8Args &a, void *part, size_t part_bytes, hipStream_t st) {
+    const Int8Plan plan = int8_plan(a.T, a.N, a.K, a.offsets ? a.E : 0, (int64_t)std::min<size_t>(part_bytes, (size_t)kInt8PartBytes));
+    switch (plan.form) {
+        case kInt8Few: return launch_int8_few(a, st);
+        case kInt8Mid32: return launch_int8_mid(a, 32, plan.splits, part, st);
+        case kInt8Mid64: return launch_int8_mid(a, 64, plan.splits, part, st);
+        case kInt8Tile128: return launch_int8_tiles(a, 128, st);
+        default: return launch_int8_tiles(a, 256, st);
+    }
 }
 
 // sizes, bits and flags of a product
@@ -140,7 +157,7 @@ Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, 
 // quantizes the tokens into the workspace and multiplies them
 mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t ws_bytes, hipStream_t st) {
     const Int8Layout l = int8_layout(a.M > a.T ? a.M : a.T, a.K);
-    if (!ws || !aligned16(ws) || ws_bytes < l.total) return MQ_ERR_WORKSPACE;
+    if (!ws || !aligned16(ws) || ws_bytes < l.part + 256) return MQ_ERR_WORKSPACE;
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
     int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
     float *scale = reinterpret_cast<float *>(base + l.scale);
@@ -156,7 +173,7 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
-    return launch_int8(a, st);
+    return launch_int8(a, base + l.part, ws_bytes - l.part - 256, st);
 }
 
 }  // namespace
@@ -168,13 +185,14 @@ mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_
     return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
 }
 
-mq_status launch_int8(const Int8Args &a, hipStream_t st) {
-    return a.T / a.E >= 96 ? launch_int8_tiles(a, st) : launch_int8_blocks(a, st);
-}
-
-size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    (void)N;
-    return K < 1 || K > kInt8MaxK ? 0 : int8_layout(M, K).total;
+size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K, bool grouped) {
+    if (K < 1 || K > kInt8MaxK) return 0;
+    size_t part = 0;
+    if (!grouped && M > 0 && N > 0) {
+        const Int8Plan plan = int8_plan(M, N, K, 0, kInt8PartBytes);
+        part = (size_t)int8_part_bytes(kInt8Costs[plan.form], M, N, plan.splits);
+    }
+    return int8_layout(M, K).part + part + 256;
 }
 
 }  // namespace mq
@@ -192,7 +210,7 @@ extern "C" mq_status mq_quantize_tokens(const uint16_t *X, int64_t M, int64_t K,
 
 extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,
                                                   const float *alpha, const float *zero, int64_t M, int64_t N, int64_t K, int r,
-                                                  uint32_t flags, uint16_t *Y, void *hip_stream) {
+                                                  uint32_t flags, uint16_t *Y, void *ws, size_t ws_bytes, void *hip_stream) {
     using namespace mq;
     mq_status s = check_int8(M, N, K, r, flags);
     if (s != MQ_OK || M == 0 || N == 0) return s;
@@ -200,11 +218,13 @@ extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float 
     s = check_weights(codes, alpha, zero, Y);
     if (s != MQ_OK) return s;
     if (!aligned16(Xq) || !aligned16(scale) || !aligned16(sum)) return MQ_ERR_ALIGN;
+    if (ws && !aligned16(ws)) return MQ_ERR_WORKSPACE;
     Int8Args a = int8_args(codes, alpha, zero, M, M, N, K, 1, r, flags, Y);
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
-    return launch_int8(a, static_cast<hipStream_t>(hip_stream));
+    uint8_t *part = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+    return launch_int8(a, part, ws && ws_bytes > 256 ? ws_bytes - 256 : 0, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t N,

@@ -1,0 +1,218 @@
+// The product in 8-bit integers between few and many tokens: small tiles through LDS, several workgroups to a compute unit, K split over
+// workgroups where there are not enough tiles.
+#include "mq_int8.h"
+#include "mq_linear.h"
+
+namespace mq {
+
+// NW waves, WR x WC of them, each with RB blocks of 16 channels times TB blocks of 16 places; stages of 128 k, NBUF of them in LDS.
+template <int RB, int TB, int WR, int WC, int NBUF>
+struct Int8Mid {
+    static constexpr int NW = WR * WC, TN = 16 * RB * WR, TM = 16 * TB * WC;
+    static constexpr int STAGE = (TN + TM) * 128, LDS = NBUF * STAGE;
+};
+
+// four neighbouring outputs (n .. n + 3) of one place, or the two gated ones
+__device__ __forceinline__ void store_four(const Int8Args &a, int place, int n, const i32x4 &dot, float scale, float sum, const f32x4 &ka,
+                                           const f32x4 &kb) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
+    if (a.gate) {
+        const uint32_t o = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
+        uint16_t *out = a.Y + (int64_t)place * (a.N / 2) + n / 2;
+        if (a.N % 4 == 0) {
+            *reinterpret_cast<uint32_t *>(out) = o;
+        } else {
+            out[0] = (uint16_t)o;
+            if (n + 2 < a.N) out[1] = (uint16_t)(o >> 16);
+        }
+    } else {
+        const u32x2 o = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        uint16_t *out = a.Y + (int64_t)place * a.N + n;
+        if (a.N % 4 == 0) {
+            *reinterpret_cast<u32x2 *>(out) = o;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < a.N) out[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+        }
+    }
+}
+__device__ __forceinline__ void load_factors(const Int8Args &a, int expert, int n, f32x4 &ka, f32x4 &kb) {
+    const float *alpha = a.alpha + (int64_t)expert * a.N, *zero = a.zero + (int64_t)expert * a.N;
+    f32x4 al, ze;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        al[e] = alpha[min(n + e, a.N - 1)];
+        ze[e] = zero[min(n + e, a.N - 1)];
+    }
+    channel_factors(al, ze, a.mult, a.offset, ka, kb);
+}
+
+struct Int8Ranges {
+    i32x4 *part;  // [split][tile][wave, rb, tb][lane]
+    int splits;
+};
+
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
+__global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    typedef Int8Mid<RB, TB, WR, WC, NBUF> T;
+    constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL;
+    static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0, "");
+    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
+    const int tiles = tiles_m * tiles_n;
+    const uint32_t wid = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const int split = (int)(wid / (uint32_t)tiles), tile = (int)(wid % (uint32_t)tiles);
+    const Block b = find_block(a, tile % tiles_m, T::TM);   // (tiles of the same channels follow each other)
+    if (b.count <= 0) return;
+    const int n0 = tile / tiles_m * T::TN;
+    const int stages = (a.K + 127) / 128;
+    const int s0 = (int)((int64_t)stages * split / s.splits), s1 = (int)((int64_t)stages * (split + 1) / s.splits);
+    const int k_end = min(a.K, s1 * 128);
+
+    const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
+    const int64_t base = a.rows ? 0 : b.place;   // (gathered tokens lie within 2 GiB)
+    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + base * a.K, (uint64_t)(a.M - base) * a.K);
+    uint32_t coff;
+    int col;
+    bf16_tile_lane<NW>(wave, lane, 0, (uint32_t)a.K, coff, col);   // (rows of eight 16-byte chunks as there)
+    col *= 2;
+    const uint32_t cstep = 8u * NW * (uint32_t)a.K;
+    uint32_t xoff[XL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+        const int row = wave * 8 + (lane >> 3) + 8 * NW * i;
+        xoff[i] = (uint32_t)(token_of(a, b.place + min(row, b.count - 1)) - (int)base) * (uint32_t)a.K + (uint32_t)col;
+    }
+    auto issue = [&](int st, int buf) {   // past the end of the range: out of range, zeros
+        const int k0 = st * 128;
+        const bool in = k0 + col < k_end;
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) {
+            const uint32_t off = i < CL ? coff + (uint32_t)i * cstep : xoff[i < CL ? 0 : i - CL];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)(smem + buf * T::STAGE + (wave + i * NW) * 1024), 16,
+                                                     in ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
+        }
+    };
+    uint32_t ca[2], xa[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int sw = ((2 * group_chunk(g4) + t) ^ ((l16 >> 1) & 7)) << 4;
+        ca[t] = (wr * 16 * RB + l16) * 128 + sw;
+        xa[t] = T::TN * 128 + (wc * 16 * TB + l16) * 128 + sw;
+    }
+    i32x4 acc[RB][TB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
+
+#pragma unroll
+    for (int i = 0; i < NBUF - 1; ++i) issue(s0 + i, i);
+    int buf = 0, free = NBUF - 1;
+    for (int st = s0; st < s1; ++st) {
+        // stage st has landed, every wave is done with stage st - 1, whose buffer is filled again
+        stage_barrier<(NBUF - 2) * LPS, 0>();
+        issue(st + NBUF - 1, free);
+        const uint8_t *at = smem + buf * T::STAGE;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            i32x4 w[RB], x[TB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) w[rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(at + ca[t] + rb * 2048));
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) x[tb] = *reinterpret_cast<const i32x4 *>(at + xa[t] + tb * 2048);
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) acc[rb][tb] = mfma_i8(w[rb], x[tb], acc[rb][tb]);
+        }
+        free = buf;
+        buf = buf + 1 == NBUF ? 0 : buf + 1;
+    }
+    wait_vm0();   // (no load may be on its way into LDS that another workgroup gets)
+    if (s.splits > 1) {
+        i32x4 *to = s.part + ((int64_t)wid * NW + wave) * (RB * TB * 64) + lane;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) to[(rb * TB + tb) * 64] = acc[rb][tb];
+        return;
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int n = n0 + (wr * RB + rb) * 16 + 4 * g4;
+        f32x4 ka, kb;
+        load_factors(a, b.expert, n, ka, kb);
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) {
+            const int row = (wc * TB + tb) * 16 + l16;
+            if (row >= b.count || n >= a.N) continue;
+            const int m = token_of(a, b.place + row);
+            store_four(a, b.place + row, n, acc[rb][tb], a.scale[m], (float)a.sum[m], ka, kb);
+        }
+    }
+#else
+    (void)a;
+#endif
+}
+
+// Adds the ranges (whole numbers: in any order) and finishes the outputs: a wave for each block of 16 channels x 16 places.  Dense products
+// only.
+template <int RB, int TB, int WR, int WC>
+__global__ __launch_bounds__(256) void int8_mid_finish_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
+    constexpr int NW = WR * WC, BLOCKS = NW * RB * TB;
+    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, id = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int tile = id / BLOCKS, wave = id % BLOCKS / (RB * TB), rb = id / TB % RB, tb = id % TB, wr = wave / WC, wc = wave % WC;
+    const int tiles = tiles_m * tiles_n;
+    if (tile >= tiles) return;
+    const int row = tile % tiles_m * (16 * TB * WC) + (wc * TB + tb) * 16 + l16, n = tile / tiles_m * (16 * RB * WR) + (wr * RB + rb) * 16 + 4 * g4;
+    if (row >= a.T || n >= a.N) return;
+    const i32x4 *from = s.part + (int64_t)id * 64 + lane;
+    const int64_t step = (int64_t)tiles * BLOCKS * 64;
+    f32x4 ka, kb;
+    load_factors(a, 0, n, ka, kb);
+    const float scale = a.scale[row], sum = (float)a.sum[row];
+    i32x4 dot = {0, 0, 0, 0};
+    for (int i = 0; i < s.splits; i += 4) {   // four loads in flight
+        i32x4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = i + j < s.splits ? from[(i + j) * step] : i32x4{0, 0, 0, 0};
+        dot += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    store_four(a, row, n, dot, scale, sum, ka, kb);
+}
+
+namespace {
+
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
+mq_status launch_mid(const Int8Args &a, int splits, void *part, hipStream_t st) {
+    typedef Int8Mid<RB, TB, WR, WC, NBUF> T;
+    const int64_t tiles_n = cdiv(a.N, T::TN), tiles_m = block_bound(a.T, a.E, a.offsets != nullptr, T::TM);
+    if (tiles_n * tiles_m * splits > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    constexpr auto kernel = int8_mid_kernel<R8, RB, TB, WR, WC, NBUF>;
+    if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;
+    const Int8Ranges s{static_cast<i32x4 *>(part), splits};
+    kernel<<<dim3((unsigned)(tiles_n * tiles_m * splits)), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n, s);
+    const mq_status status = launch_status();
+    if (status != MQ_OK || splits == 1) return status;
+    int8_mid_finish_kernel<RB, TB, WR, WC><<<dim3((unsigned)cdiv(tiles_n * tiles_m * T::NW * RB * TB, 4)), dim3(256), 0, st>>>(a, (int)tiles_m, (int)tiles_n, s);
+    return launch_status();
+}
+
+template <int RB, int TB, int WR, int WC, int NBUF>
+mq_status launch_mid_form(const Int8Args &a, int splits, void *part, hipStream_t st) {
+    return a.offset != 0.f ? launch_mid<true, RB, TB, WR, WC, NBUF>(a, splits, part, st) : launch_mid<false, RB, TB, WR, WC, NBUF>(a, splits, part, st);
+}
+
+}  // namespace
+
+mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st) {
+    return places == 32 ? launch_mid_form<1, 2, 4, 1, 4>(a, splits, part, st) : launch_mid_form<1, 4, 4, 1, 4>(a, splits, part, st);
+}
+
+}  // namespace mq

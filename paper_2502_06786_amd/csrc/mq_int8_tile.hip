@@ -263,11 +263,9 @@ mq_status launch_tile(const Int8Args &a, hipStream_t st) {
 
 }  // namespace
 
-#ifndef MQ_TILE
-#define MQ_TILE 4, 8, 4, 2, 1
-#endif
-mq_status launch_int8_tiles(const Int8Args &a, hipStream_t st) {
-    return a.offset != 0.f ? launch_tile<true, MQ_TILE>(a, st) : launch_tile<false, MQ_TILE>(a, st);
+mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st) {
+    if (places == 128) return a.offset != 0.f ? launch_tile<true, 4, 4, 2, 2, 2>(a, st) : launch_tile<false, 4, 4, 2, 2, 2>(a, st);
+    return a.offset != 0.f ? launch_tile<true, 4, 8, 4, 2, 1>(a, st) : launch_tile<false, 4, 8, 4, 2, 1>(a, st);
 }
 
 }  // namespace mq

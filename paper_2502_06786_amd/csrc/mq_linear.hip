@@ -1073,7 +1073,7 @@ extern "C" size_t mq_workspace_bytes(int op, int64_t M, int64_t N, int64_t K, in
     if (op == MQ_OP_L2_LOSS) return loss_workspace_bytes(M, N);
     if (op == MQ_OP_LINEAR_BWD_CLIP) return clip_workspace_bytes(M, N, K, nr);
     if (op == MQ_OP_AFFINE_BWD) return affine_workspace_bytes(M, N, K);
-    if (op == MQ_OP_LINEAR_FWD_INT8 || op == MQ_OP_EXPERTS_FWD_INT8) return int8_workspace_bytes(M, N, K);
+    if (op == MQ_OP_LINEAR_FWD_INT8 || op == MQ_OP_EXPERTS_FWD_INT8) return int8_workspace_bytes(M, N, K, op == MQ_OP_EXPERTS_FWD_INT8);
     if (op == MQ_OP_EXPERTS_ROUTE) return route_workspace_bytes(M, N);
     return 0;
 }

@@ -22,7 +22,7 @@ def lib():
     vp, i64, ci, u32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_uint32, ctypes.c_size_t
     lib_.mq_quantize_tokens.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp]
     lib_.mq_linear_fwd_int8.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp, sz, vp]
-    lib_.mq_linear_fwd_int8_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp]
+    lib_.mq_linear_fwd_int8_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, u32, vp, vp, sz, vp]
     lib_.mq_experts_route.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     lib_.mq_experts_fwd_int8.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, u32, vp, vp, sz, vp]
     lib_.mq_experts_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp]
@@ -45,8 +45,8 @@ def test_linear(lib):
     def f(X=P, codes=P, alpha=P, zero=P, M=4, N=32, K=64, r=8, flags=0, Y=P, ws=P, ws_bytes=1 << 30):
         return lib.mq_linear_fwd_int8(X, codes, alpha, zero, M, N, K, r, flags, Y, ws, ws_bytes, None)
 
-    def q(Xq=P, scale=P, sums=P, codes=P, alpha=P, zero=P, M=4, N=32, K=64, r=8, flags=0, Y=P):
-        return lib.mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, M, N, K, r, flags, Y, None)
+    def q(Xq=P, scale=P, sums=P, codes=P, alpha=P, zero=P, M=4, N=32, K=64, r=8, flags=0, Y=P, ws=None, ws_bytes=0):
+        return lib.mq_linear_fwd_int8_quantized(Xq, scale, sums, codes, alpha, zero, M, N, K, r, flags, Y, ws, ws_bytes, None)
     for g in (f, q):
         assert g(M=-1) == g(N=-1) == g(K=0) == g(K=131088) == g(M=(1 << 31) - 255) == g(N=(1 << 31) - 255) == SHAPE
         assert g(r=0) == g(r=9) == BITS
@@ -58,8 +58,9 @@ def test_linear(lib):
     assert f(X=None) == NULL and f(X=ODD) == ALIGN
     assert q(Xq=None) == q(scale=None) == q(sums=None) == NULL
     assert q(Xq=ODD) == q(scale=ODD) == q(sums=ODD) == ALIGN
+    assert q(ws=ODD, ws_bytes=1 << 20) == WORKSPACE
     assert f(ws=None) == f(ws_bytes=16) == f(ws=ODD) == WORKSPACE
-    need = lib.mq_workspace_bytes(8, 4, 32, 64, 1)
+    need = lib.mq_workspace_bytes(8, 4, 32, 64, 1)   # (at this size K is not cut)
     assert f(ws_bytes=need - 1) == WORKSPACE
 
 
@@ -99,7 +100,9 @@ def test_workspaces(lib):
     for op in (8, 10):
         assert f(op, 100, 64, 4096, 1) >= 100 * 4096 + 800
         assert f(op, 100, 64, 131088, 1) == 0 and f(op, -1, 64, 64, 1) == 0 and f(op, 100, 64, 0, 1) == 0
-        assert f(op, 100, 64, 4096, 1) <= f(op, 101, 64, 4096, 1)
+    assert f(10, 100, 64, 4096, 1) <= f(10, 101, 64, 4096, 1)
+    assert f(8, 77, 4096, 14336, 1) > f(10, 77, 4096, 14336, 1)      # partial sums
+    assert f(8, 4000, 14336, 4096, 1) == f(10, 4000, 14336, 4096, 1)
     assert f(9, 5000, 64, 0, 1) >= 2 * 65 * 4 and f(9, 5000, 0, 0, 1) == 0 and f(9, 5000, 1025, 0, 1) == 0
 
 
