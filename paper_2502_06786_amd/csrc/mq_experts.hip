@@ -202,7 +202,7 @@ extern "C" mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place,
     const CombineArgs a{Y, place, weight, out, M, N, (int)top, (int)T};
     const int V = N % 8 == 0 ? 8 : 1;
     const int64_t blocks = cdiv(M * (N / V), 256);
-    if (blocks > 0x7FFFFFFF) return MQ_ERR_SHAPE;
+    if (blocks > 0xFFFFFF) return MQ_ERR_SHAPE;   // (a launch has less than 2^32 threads)
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (V == 8)
         combine_kernel<8><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);

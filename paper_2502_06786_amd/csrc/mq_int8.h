@@ -60,49 +60,136 @@ __device__ __forceinline__ float gated_value(float g, float u, int gate) {
     return g * __builtin_amdgcn_rcpf(1.0f + __expf(-t)) * u;
 }
 
-// The `block`-th block of BM places, counted expert by expert: no block holds places of two experts.
+// ---- a token's codes: scale = top / 127, code = round(x (127 / top)), top the row's largest magnitude -------------------------------
+// The largest magnitude is found on the bf16 bits themselves: their order is that of the magnitudes, infinities and NaN last.
+__device__ __forceinline__ uint32_t top_of(uint32_t top2, const u32x4 &v) {   // largest so far of the low and of the high halves
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+        top2 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top2), __builtin_bit_cast(u16x2, v[w] & 0x7FFF7FFFu)));
+    return top2;
+}
+__device__ __forceinline__ uint32_t top_of_wave(uint32_t top2) {
+    uint32_t top = max(top2 & 0xFFFFu, top2 >> 16);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    return top;
+}
+struct TokenScale {
+    float lift, per, scale;
+    bool finite;
+};
+__device__ __forceinline__ TokenScale token_scale(uint32_t top) {
+    const bool finite = top < 0x7F80u;
+    const float most = bf16_bits_to_float(top);
+    const float lift = most < 0x1p-100f ? 0x1p100f : 1.0f;          // 127 / most would pass the largest fp32 number
+    return {lift, finite && top != 0 ? __fdiv_rn(127.0f, most * lift) : 0.0f, finite ? __fdiv_rn(most, 127.0f) : __uint_as_float(0x7FC00000u), finite};
+}
+// eight values -> eight codes; their sum is added to total
+__device__ __forceinline__ u32x2 token_codes(const u32x4 &v, const TokenScale &t, int &total) {
+    uint32_t out[2] = {0u, 0u};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t d = t.finite ? v[w] : 0u;  // (infinity times zero is no number)
+        const int lo = (int)rintf(bf16_lo(d) * t.lift * t.per), hi = (int)rintf(bf16_hi(d) * t.lift * t.per);
+        total += lo + hi;
+        out[w >> 1] |= ((uint32_t)(lo & 0xFF) | (uint32_t)(hi & 0xFF) << 8) << (16 * (w & 1));
+    }
+    return u32x2{out[0], out[1]};
+}
+__device__ __forceinline__ int sum_of_wave(int total) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    return total;
+}
+
+// The `block`-th block of BM places, counted expert by expert: no block holds places of two experts.  `bound(e)`: where the places of
+// expert e begin, e = 0 .. E (data: whatever it holds, places stay below T).
 struct Block {
     int expert, place, count;  // count = 0: there is no such block
 };
-__device__ __forceinline__ Block find_block(const Int8Args &a, int block, int BM) {
-    if (!a.offsets) return Block{0, block * BM, min(BM, a.T - block * BM)};
-    // a lane for each expert: blocks up to and with it by a prefix sum.  (Offsets are data: whatever they hold, places stay below T.)
+template <typename Bound>
+__device__ __forceinline__ Block find_block(int T, int E, int block, int BM, Bound &&bound, int *blocks = nullptr) {
+    // a lane for each expert: blocks up to and with it by a prefix sum
     const int lane = threadIdx.x & 63;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
+    Block found{0, 0, 0};
+    int before = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
         const int e = e0 + lane;
         int lo = 0, hi = 0;
-        if (e < a.E) {
-            lo = min(max(a.offsets[e], 0), a.T);
-            hi = min(max(a.offsets[e + 1], lo), a.T);
+        if (e < E) {
+            lo = min(max(bound(e), 0), T);
+            hi = min(max(bound(e + 1), lo), T);
         }
         const int mine = (int)(((uint32_t)(hi - lo) + (uint32_t)BM - 1u) / (uint32_t)BM);
-        int upto = mine;
+        int upto = before + mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o, 64);
+            const int v = __shfl_up(upto, o, 64) - before;
             if (lane >= o) upto += v;
         }
         const uint64_t past = __ballot(upto > block);
-        if (past) {
+        if (past && found.count == 0) {
             const int at = __builtin_ctzll(past);
-            const int first = __builtin_amdgcn_readfirstlane(__shfl(upto - mine, at, 64));
-            const int place = __builtin_amdgcn_readfirstlane(__shfl(lo, at, 64)) + (block - first) * BM;
-            const int end = __builtin_amdgcn_readfirstlane(__shfl(hi, at, 64));
-            return Block{e0 + at, place, min(BM, end - place)};
+            const int first = __builtin_amdgcn_readlane(upto - mine, at), place = __builtin_amdgcn_readlane(lo, at) + (block - first) * BM;
+            found = Block{e0 + at, place, min(BM, __builtin_amdgcn_readlane(hi, at) - place)};
+            if (!blocks) return found;
         }
-        block -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
+        before = __builtin_amdgcn_readlane(upto, 63);
     }
-    return Block{0, 0, 0};
+    if (blocks) *blocks = before;
+    return found;
 }
-// blocks of a launch, at most
-inline int64_t block_bound(int64_t T, int64_t E, bool grouped, int BM) { return grouped ? T / BM + (E < T ? E : T) : cdiv(T, BM); }
-
+__device__ __forceinline__ Block find_block(const Int8Args &a, int block, int BM) {
+    if (!a.offsets) return Block{0, block * BM, min(BM, a.T - block * BM)};
+    return find_block(a.T, a.E, block, BM, [&](int e) { return a.offsets[e]; });
+}
 // the token of a place (rows are data: whatever they hold, tokens stay below M)
 __device__ __forceinline__ int token_of(const Int8Args &a, int place) { return a.rows ? min(max(a.rows[place], 0), a.M - 1) : place; }
+
+// four neighbouring outputs (n .. n + 3) of one place, or the two gated ones
+__device__ __forceinline__ void store_four(const Int8Args &a, int place, int n, const i32x4 &dot, float scale, float sum, const f32x4 &ka,
+                                           const f32x4 &kb) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
+    if (a.gate) {
+        const uint32_t o = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
+        uint16_t *out = a.Y + (int64_t)place * (a.N / 2) + n / 2;
+        if (a.N % 4 == 0) {
+            *reinterpret_cast<uint32_t *>(out) = o;
+        } else {
+            out[0] = (uint16_t)o;
+            if (n + 2 < a.N) out[1] = (uint16_t)(o >> 16);
+        }
+    } else {
+        const u32x2 o = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        uint16_t *out = a.Y + (int64_t)place * a.N + n;
+        if (a.N % 4 == 0) {
+            *reinterpret_cast<u32x2 *>(out) = o;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < a.N) out[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+        }
+    }
+}
+
+__device__ __forceinline__ void load_factors(const Int8Args &a, int expert, int n, f32x4 &ka, f32x4 &kb) {
+    const float *alpha = a.alpha + (int64_t)expert * a.N, *zero = a.zero + (int64_t)expert * a.N;
+    f32x4 al, ze;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        al[e] = alpha[min(n + e, a.N - 1)];
+        ze[e] = zero[min(n + e, a.N - 1)];
+    }
+    channel_factors(al, ze, a.mult, a.offset, ka, kb);
+}
 
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
                                  float *scale, int32_t *sum, hipStream_t st);
 mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
+// the same on bf16 tokens X [M, K], for up to kInt8SinglePlaces places and kInt8SingleK values a token
+mq_status launch_int8_single(const Int8Args &a, const uint16_t *X, hipStream_t st);
 // places: of a tile, 32 or 64; part: room for the partial sums of `splits` ranges of K
 mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st);
 // places: of a tile, 128 or 256

@@ -9,15 +9,12 @@ namespace mq {
 // ============================================================================================
 // quantizer of tokens
 // ============================================================================================
-// scale = top / 127, code = round(x (127 / top)) with top the row's largest magnitude, sum = the row's codes added up.  One read of the
-// row into registers, so 2 bytes read and 1 written per value; the largest magnitude is found on the bf16 bits themselves (their order is
-// that of the magnitudes, infinities and NaN last).
-// TPR threads to a row, V chunks of 8 values in each.
+// One read of the row into registers, so 2 bytes read and 1 written per value.  TPR threads to a row, V chunks of 8 values in each.
 // rows: null, or the row of X that row m of the result is made of (rows are data: whatever they hold, they stay below X_rows).
 template <int TPR, int V, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *__restrict__ X, int64_t M, int K, int64_t ldx,
-                                                                const int32_t *__restrict__ rows, int X_rows, int8_t *__restrict__ Xq, float *__restrict__ scale,
-                                                                int32_t *__restrict__ sum) {
+                                                                const int32_t *__restrict__ rows, int X_rows, int8_t *__restrict__ Xq,
+                                                                float *__restrict__ scale, int32_t *__restrict__ sum) {
     constexpr int WAVES = TPR / 64;  // to a row
     __shared__ uint32_t tops[BLOCK / 64];
     __shared__ int32_t sums[BLOCK / 64];
@@ -28,48 +25,31 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
     if (rows) from = min(max(rows[from], 0), X_rows - 1);
     const u32x4 *src = reinterpret_cast<const u32x4 *>(X + from * ldx);
     u32x4 v[V];
-    uint32_t top2 = 0;  // largest magnitude of the low and of the high halves
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         v[i] = u32x4{0u, 0u, 0u, 0u};
         const int c = t + i * TPR;
         if (live && c * 8 < K) v[i] = src[c];
     }
+    uint32_t top2 = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            top2 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top2),
-                                                                          __builtin_bit_cast(u16x2, v[i][w] & 0x7FFF7FFFu)));
-    uint32_t top = max(top2 & 0xFFFFu, top2 >> 16);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    for (int i = 0; i < V; ++i) top2 = top_of(top2, v[i]);
+    uint32_t top = top_of_wave(top2);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) tops[wave] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = max(top, tops[first + w]);
     }
-    const bool finite = top < 0x7F80u;
-    const float most = bf16_bits_to_float(top);
-    const float lift = most < 0x1p-100f ? 0x1p100f : 1.0f;          // 127 / most would pass the largest fp32 number
-    const float per = finite && top != 0 ? __fdiv_rn(127.0f, most * lift) : 0.0f;
+    const TokenScale ts = token_scale(top);
     int total = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int c = t + i * TPR;
-        uint32_t out[2] = {0u, 0u};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t d = finite ? v[i][w] : 0u;  // (infinity times zero is no number)
-            const int lo = (int)rintf(bf16_lo(d) * lift * per), hi = (int)rintf(bf16_hi(d) * lift * per);
-            total += lo + hi;
-            out[w >> 1] |= ((uint32_t)(lo & 0xFF) | (uint32_t)(hi & 0xFF) << 8) << (16 * (w & 1));
-        }
-        if (live && c * 8 < K) *reinterpret_cast<u32x2 *>(Xq + m * K + c * 8) = u32x2{out[0], out[1]};
+        const u32x2 codes = token_codes(v[i], ts, total);
+        if (live && c * 8 < K) *reinterpret_cast<u32x2 *>(Xq + m * K + c * 8) = codes;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    total = sum_of_wave(total);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) sums[wave] = total;
         __syncthreads();
@@ -78,7 +58,7 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
         for (int w = 0; w < WAVES; ++w) total += sums[first + w];
     }
     if (live && t == 0) {
-        scale[m] = finite ? __fdiv_rn(most, 127.0f) : __uint_as_float(0x7FC00000u);
+        scale[m] = ts.scale;
         sum[m] = total;
     }
 }
@@ -88,7 +68,13 @@ namespace {
 template <int TPR, int V, int BLOCK>
 mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, float *scale,
                         int32_t *sum, hipStream_t st) {
-    quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(M, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(X, M, (int)K, ldx, rows, (int)X_rows, Xq, scale, sum);
+    // (a launch has less than 2^32 threads)
+    constexpr int64_t most = 0xFFFFFFFFll / BLOCK * (BLOCK / TPR);
+    for (int64_t m = 0; m < M; m += most) {
+        const int64_t n = std::min(M - m, most);
+        quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(n, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(
+            rows ? X : X + m * ldx, n, (int)K, ldx, rows ? rows + m : nullptr, (int)X_rows, Xq + m * K, scale + m, sum + m);
+    }
     return launch_status();
 }
 
@@ -158,6 +144,7 @@ Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, 
 mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t ws_bytes, hipStream_t st) {
     const Int8Layout l = int8_layout(a.M > a.T ? a.M : a.T, a.K);
     if (!ws || !aligned16(ws) || ws_bytes < l.part + 256) return MQ_ERR_WORKSPACE;
+    if (int8_single(a.T, a.N, a.K, a.offsets ? a.E : 0)) return launch_int8_single(a, X, st);
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
     int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
     float *scale = reinterpret_cast<float *>(base + l.scale);

@@ -1,130 +1,213 @@
 // The product in 8-bit integers for few tokens: bound by the codes' way out of memory.
-#include <type_traits>
+#include <algorithm>
 
 #include "mq_int8.h"
 #include "mq_linear.h"
 
 namespace mq {
 
-// Workgroup = up to 16 TB places x 16 RB channels of one expert; its NW waves take turns along K, 128 bytes of every row at a time, and
-// add their sums (whole numbers) in LDS.  Operands go straight from memory to registers, U turns at once.  Rows of the matrix-core product
-// are channels, columns places: lane (l16, g4) ends up with channels 4 g4 .. 4 g4 + 3 of place l16.
-template <bool R8, int RB, int TB, int NW, int U>
+// Workgroup = up to 16 places x 16 channels of one expert; its NW waves take turns along K, 128 bytes of every row at a time, and add
+// their sums (whole numbers) in LDS.  Operands go straight from memory to registers, DEEP turns ahead.  Rows of the matrix-core product are
+// channels, columns places: lane (l16, g4) ends up with channels 4 g4 .. 4 g4 + 3 of place l16.
+template <bool R8, int NW, int DEEP>
 __global__ __launch_bounds__(64 * NW) void int8_few_kernel(Int8Args a, int tiles_n, int blocks) {
-    __shared__ i32x4 part[NW][RB * TB][64];
+    __shared__ i32x4 part[NW][64];
     const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lid = xcd_contiguous_id(blockIdx.x, gridDim.x);   // (blocks of one expert follow each other: its codes are in that L2)
-    const Block b = find_block(a, (int)(lid % (uint32_t)blocks), 16 * TB);
+    const Block b = find_block(a, (int)(lid % (uint32_t)blocks), 16);
+    if (b.count <= 0) return;
+    const int n0 = (int)(lid / (uint32_t)blocks) * 16;
+
+    const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
+    const int base = a.rows ? 0 : b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
+    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + (int64_t)base * a.K, (uint64_t)(a.M - base) * a.K);
+    const int m = token_of(a, b.place + min(l16, b.count - 1));
+    // (a lane takes 32 neighbouring bytes of a row, so that the four of a row take a line; both operands in that order)
+    const uint32_t coff = (uint32_t)l16 * (uint32_t)a.K + 32u * g4, xoff = (uint32_t)(m - base) * (uint32_t)a.K + 32u * g4;
+    i32x4 c[DEEP][2], x[DEEP][2];
+    auto load = [&](int slot, int k0) {   // past the end of the rows: out of range, zeros
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + 16 * h;
+            const bool in = k + 32 * g4 < a.K;
+            c[slot][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rC, in ? coff + (uint32_t)k : kOOB, 0, 0));
+            x[slot][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rX, in ? xoff + (uint32_t)k : kOOB, 0, 0));
+        }
+    };
+    constexpr int TURN = 128 * NW;
+    int k0 = wave * 128;
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) load(u, k0 + u * TURN);
+
+    // what the outputs need, requested behind the first operands
+    const int n = n0 + 4 * g4;
+    float alpha[4], zero[4], scale = 0.f;
+    int total = 0;
+    if (wave == 0) {
+        const int64_t first = (int64_t)b.expert * a.N;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            alpha[e] = a.alpha[first + min(n + e, a.N - 1)];
+            zero[e] = a.zero[first + min(n + e, a.N - 1)];
+        }
+        scale = a.scale[m];
+        total = a.sum[m];
+    }
+    i32x4 acc = {0, 0, 0, 0};
+    for (; k0 < a.K; k0 += DEEP * TURN)
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc = mfma_i8(signed_codes<R8>(c[u][h]), x[u][h], acc);
+            if (k0 + DEEP * TURN < a.K) load(u, k0 + (DEEP + u) * TURN);
+        }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0 || l16 >= b.count || n >= a.N) return;
+    f32x4 ka, kb;
+    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, a.offset, ka, kb);
+#pragma unroll
+    for (int w = 1; w < NW; ++w) acc += part[w][lane];
+    store_four(a, b.place + l16, n, acc, scale, (float)total, ka, kb);
+}
+
+// The same on bf16 tokens, which every workgroup quantizes for itself into LDS while its first codes are on their way: up to
+// kInt8SinglePlaces places in all.  Workgroup = 16 RB channels, four waves.
+template <bool R8, int RB, int DEEP>
+__global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint16_t *__restrict__ X, int tiles_n, int blocks) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];   // codes [count][K + 16]
+    constexpr int NW = 4, V = kInt8SingleK / (8 * 64 * NW);
+    __shared__ i32x4 part[NW][RB][64];
+    __shared__ uint32_t tops[NW];
+    __shared__ int32_t sums[kInt8SinglePlaces][NW];
+    __shared__ float scales[kInt8SinglePlaces];
+    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lid = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const Block b = find_block(a, (int)(lid % (uint32_t)blocks), 16);
     if (b.count <= 0) return;
     const int n0 = (int)(lid / (uint32_t)blocks) * 16 * RB;
 
     const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
-    const int64_t base = a.rows ? 0 : b.place;   // (gathered tokens lie within 2 GiB)
-    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + base * a.K, (uint64_t)(a.M - base) * a.K);
-    // (a lane takes 32 neighbouring bytes of a row, so that the four of a row take a line; both operands in that order)
     const uint32_t coff = (uint32_t)l16 * (uint32_t)a.K + 32u * g4;
-    uint32_t xoff[TB];
+    i32x4 c[DEEP][RB][2];
+    auto load = [&](int slot, int k0) {   // past the end of the rows: out of range, zeros
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb)
-        xoff[tb] = (uint32_t)(token_of(a, b.place + min(16 * tb + l16, b.count - 1)) - (int)base) * (uint32_t)a.K + 32u * g4;
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + 16 * h;
+                const bool in = k + 32 * g4 < a.K;
+                c[slot][rb][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                               rC, in ? coff + (uint32_t)(16 * rb) * (uint32_t)a.K + (uint32_t)k : kOOB, 0, 0));
+            }
+    };
+    constexpr int TURN = 128 * NW;
+    int k0 = wave * 128;
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) load(u, k0 + u * TURN);
 
-    i32x4 acc[RB][TB];
+    const int row_bytes = a.K + 16;
+    for (int j = 0; j < b.count; ++j) {
+        const u32x4 *src = reinterpret_cast<const u32x4 *>(X + (int64_t)token_of(a, b.place + j) * a.K);
+        u32x4 v[V];
+        uint32_t top2 = 0;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
-    auto turns = [&](auto inside_tag, int k0) {   // U turns from k0 on
-        constexpr bool INSIDE = decltype(inside_tag)::value;
-        i32x4 c[U][RB][2], x[U][TB][2];
-        auto load = [&](const __amdgpu_buffer_rsrc_t &r, uint32_t off, int k, int half) {
-            // past the end of the rows: out of range, zeros
-            if constexpr (INSIDE) return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16u * half, k, 0));
-            const bool in = k + 32 * g4 + 16 * half < a.K;
-            return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, in ? off + (uint32_t)k + 16u * half : kOOB, 0, 0));
-        };
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) c[u][rb][h] = load(rC, coff + (uint32_t)(16 * rb) * (uint32_t)a.K, k0 + u * 128 * NW, h);
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) x[u][tb][h] = load(rX, xoff[tb], k0 + u * 128 * NW, h);
+        for (int i = 0; i < V; ++i) {
+            v[i] = u32x4{0u, 0u, 0u, 0u};
+            if ((int)(threadIdx.x + i * 256) * 8 < a.K) v[i] = src[threadIdx.x + i * 256];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int i = 0; i < V; ++i) top2 = top_of(top2, v[i]);
+        uint32_t top = top_of_wave(top2);
+        if (j > 0) __syncthreads();   // (tops of the token before have been read)
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int w = 0; w < NW; ++w) top = max(top, tops[w]);
+        const TokenScale ts = token_scale(top);
+        int total = 0;
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const i32x4 w = signed_codes<R8>(c[u][rb][h]);
-#pragma unroll
-                    for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = mfma_i8(w, x[u][tb][h], acc[rb][tb]);
-                }
-    };
-    int k0 = wave * 128;
-    for (; k0 + (U - 1) * 128 * NW + 128 <= a.K; k0 += U * 128 * NW) turns(std::true_type{}, k0);
-    if (k0 < a.K) turns(std::false_type{}, k0);
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb) part[wave][rb * TB + tb][lane] = acc[rb][tb];
+        for (int i = 0; i < V; ++i) {
+            const int chunk = threadIdx.x + i * 256;
+            if (chunk * 8 >= a.K) break;
+            *reinterpret_cast<u32x2 *>(smem + j * row_bytes + chunk * 8) = token_codes(v[i], ts, total);
+        }
+        total = sum_of_wave(total);
+        if (lane == 0) sums[j][wave] = total;
+        if (threadIdx.x == 0) scales[j] = ts.scale;
+    }
     __syncthreads();
 
-    for (int block = wave; block < RB * TB; block += NW) {
-        const int rb = block / TB, tb = block % TB, row = 16 * tb + l16, n = n0 + 16 * rb + 4 * g4;
-        if (row >= b.count || n >= a.N) continue;
-        const int m = token_of(a, b.place + row);
-        const float scale = a.scale[m], sum = (float)a.sum[m];
-        const float *alpha = a.alpha + (int64_t)b.expert * a.N, *zero = a.zero + (int64_t)b.expert * a.N;
-        f32x4 al, ze, ka, kb;
+    i32x4 acc[RB];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            al[e] = alpha[min(n + e, a.N - 1)];
-            ze[e] = zero[min(n + e, a.N - 1)];
-        }
-        channel_factors(al, ze, a.mult, a.offset, ka, kb);
-        i32x4 dot = {0, 0, 0, 0};
+    for (int rb = 0; rb < RB; ++rb) acc[rb] = i32x4{0, 0, 0, 0};
+    const int row = min(l16, b.count - 1);
+    for (; k0 < a.K; k0 += DEEP * TURN)
 #pragma unroll
-        for (int w = 0; w < NW; ++w) dot += part[w][block][lane];
-        float y[4];
+        for (int u = 0; u < DEEP; ++u) {
+            const int k = k0 + u * TURN + 32 * g4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
-        if (a.gate) {
-            uint16_t *out = a.Y + (int64_t)(b.place + row) * (a.N / 2) + n / 2;
+            for (int h = 0; h < 2; ++h) {
+                i32x4 x = {0, 0, 0, 0};
+                if (k + 16 * h < a.K) x = *reinterpret_cast<const i32x4 *>(smem + row * row_bytes + k + 16 * h);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (n + 2 * e < a.N) out[e] = (uint16_t)float_to_bf16_bits(gated_value(y[2 * e], y[2 * e + 1], a.gate));
-        } else {
-            uint16_t *out = a.Y + (int64_t)(b.place + row) * a.N + n;
-            if (a.N % 4 == 0) {
-                *reinterpret_cast<u32x2 *>(out) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < a.N) out[e] = (uint16_t)float_to_bf16_bits(y[e]);
+                for (int rb = 0; rb < RB; ++rb) acc[rb] = mfma_i8(signed_codes<R8>(c[u][rb][h]), x, acc[rb]);
             }
+            if (k0 + DEEP * TURN < a.K) load(u, k0 + (DEEP + u) * TURN);
         }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) part[wave][rb][lane] = acc[rb];
+    __syncthreads();
+    const int n = n0 + 16 * wave + 4 * g4;
+    if (wave >= RB || l16 >= b.count || n >= a.N) return;
+    f32x4 ka, kb;
+    load_factors(a, b.expert, n, ka, kb);
+    i32x4 dot = {0, 0, 0, 0};
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        dot += part[w][wave][lane];
+        total += sums[l16][w];
     }
+    store_four(a, b.place + l16, n, dot, scales[l16], (float)total, ka, kb);
 }
 
 namespace {
 
-template <bool R8, int RB, int TB, int NW, int U>
+template <int NW, int DEEP>
 mq_status launch_few(const Int8Args &a, hipStream_t st) {
-    const int64_t tiles_n = cdiv(a.N, 16 * RB), blocks = block_bound(a.T, a.E, a.offsets != nullptr, 16 * TB);
-    if (tiles_n * blocks > 0x7FFFFF00) return MQ_ERR_SHAPE;
-    int8_few_kernel<R8, RB, TB, NW, U><<<dim3((unsigned)(tiles_n * blocks)), dim3(64 * NW), 0, st>>>(a, (int)tiles_n, (int)blocks);
+    const int64_t tiles_n = cdiv(a.N, 16), grid_size = int8_grid(kInt8Few, a.T, a.N, a.offsets ? a.E : 0, 1), blocks = grid_size / tiles_n;
+    if (grid_size > kInt8MostWorkgroups) return MQ_ERR_SHAPE;
+    const dim3 grid((unsigned)grid_size), threads(64 * NW);
+    static_assert(NW <= 4, "");
+    if (a.offset != 0.f)
+        int8_few_kernel<true, NW, DEEP><<<grid, threads, 0, st>>>(a, (int)tiles_n, (int)blocks);
+    else
+        int8_few_kernel<false, NW, DEEP><<<grid, threads, 0, st>>>(a, (int)tiles_n, (int)blocks);
+    return launch_status();
+}
+
+template <int RB, int DEEP>
+mq_status launch_single(const Int8Args &a, const uint16_t *X, hipStream_t st) {
+    const int64_t tiles_n = cdiv(a.N, 16 * RB), blocks = a.offsets ? std::min(a.T, a.E) : 1;   // (an expert has one block at most)
+    const int lds = a.T * (a.K + 16);
+    const dim3 grid((unsigned)(tiles_n * blocks));
+    if (!(a.offset != 0.f ? allow_lds<int8_single_kernel<true, RB, DEEP>>(lds) : allow_lds<int8_single_kernel<false, RB, DEEP>>(lds))) return MQ_ERR_DEVICE;
+    if (a.offset != 0.f)
+        int8_single_kernel<true, RB, DEEP><<<grid, dim3(256), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
+    else
+        int8_single_kernel<false, RB, DEEP><<<grid, dim3(256), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
     return launch_status();
 }
 
 }  // namespace
 
-mq_status launch_int8_few(const Int8Args &a, hipStream_t st) {
-    return a.offset != 0.f ? launch_few<true, 1, 1, 8, 4>(a, st) : launch_few<false, 1, 1, 8, 4>(a, st);
+mq_status launch_int8_single(const Int8Args &a, const uint16_t *X, hipStream_t st) {
+    return int8_single_wide(a.T, a.N, a.offsets ? a.E : 0) ? launch_single<2, 2>(a, X, st) : launch_single<1, 4>(a, X, st);
 }
+
+mq_status launch_int8_few(const Int8Args &a, hipStream_t st) { return launch_few<4, 8>(a, st); }
 
 }  // namespace mq

@@ -12,44 +12,6 @@ struct Int8Mid {
     static constexpr int STAGE = (TN + TM) * 128, LDS = NBUF * STAGE;
 };
 
-// four neighbouring outputs (n .. n + 3) of one place, or the two gated ones
-__device__ __forceinline__ void store_four(const Int8Args &a, int place, int n, const i32x4 &dot, float scale, float sum, const f32x4 &ka,
-                                           const f32x4 &kb) {
-    float y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
-    if (a.gate) {
-        const uint32_t o = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
-        uint16_t *out = a.Y + (int64_t)place * (a.N / 2) + n / 2;
-        if (a.N % 4 == 0) {
-            *reinterpret_cast<uint32_t *>(out) = o;
-        } else {
-            out[0] = (uint16_t)o;
-            if (n + 2 < a.N) out[1] = (uint16_t)(o >> 16);
-        }
-    } else {
-        const u32x2 o = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-        uint16_t *out = a.Y + (int64_t)place * a.N + n;
-        if (a.N % 4 == 0) {
-            *reinterpret_cast<u32x2 *>(out) = o;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.N) out[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
-        }
-    }
-}
-__device__ __forceinline__ void load_factors(const Int8Args &a, int expert, int n, f32x4 &ka, f32x4 &kb) {
-    const float *alpha = a.alpha + (int64_t)expert * a.N, *zero = a.zero + (int64_t)expert * a.N;
-    f32x4 al, ze;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        al[e] = alpha[min(n + e, a.N - 1)];
-        ze[e] = zero[min(n + e, a.N - 1)];
-    }
-    channel_factors(al, ze, a.mult, a.offset, ka, kb);
-}
-
 struct Int8Ranges {
     i32x4 *part;  // [split][tile][wave, rb, tb][lane]
     int splits;
@@ -192,12 +154,14 @@ namespace {
 template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
 mq_status launch_mid(const Int8Args &a, int splits, void *part, hipStream_t st) {
     typedef Int8Mid<RB, TB, WR, WC, NBUF> T;
-    const int64_t tiles_n = cdiv(a.N, T::TN), tiles_m = block_bound(a.T, a.E, a.offsets != nullptr, T::TM);
-    if (tiles_n * tiles_m * splits > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    const int64_t tiles_n = cdiv(a.N, T::TN), grid = int8_grid(T::TM == 32 ? kInt8Mid32 : kInt8Mid64, a.T, a.N, a.offsets ? a.E : 0, splits);
+    const int64_t tiles_m = grid / tiles_n / splits;
+    if (grid > kInt8MostWorkgroups) return MQ_ERR_SHAPE;
+    static_assert(T::NW <= 4 && T::TN == 64 && (T::TM == 32 || T::TM == 64), "the forms of mq_int8_plan.h");
     constexpr auto kernel = int8_mid_kernel<R8, RB, TB, WR, WC, NBUF>;
     if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;
     const Int8Ranges s{static_cast<i32x4 *>(part), splits};
-    kernel<<<dim3((unsigned)(tiles_n * tiles_m * splits)), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n, s);
+    kernel<<<dim3((unsigned)grid), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n, s);
     const mq_status status = launch_status();
     if (status != MQ_OK || splits == 1) return status;
     int8_mid_finish_kernel<RB, TB, WR, WC><<<dim3((unsigned)cdiv(tiles_n * tiles_m * T::NW * RB * TB, 4)), dim3(256), 0, st>>>(a, (int)tiles_m, (int)tiles_n, s);

@@ -29,8 +29,8 @@ constexpr Int8Cost kInt8Costs[kInt8Forms] = {
     {16, 16, 3, false, 1.82, 1.46, 0.091, 0.328, 5.2e6, 0, 1},
     {64, 32, 3, false, 3.60, 0.25, 0.180, 0.449, 7.2e6, 1.64, 5.2e6},
     {64, 64, 2, false, 3.87, 0.53, 0.245, 0.494, 6.4e6, 1.16, 5.9e6},
-    {128, 128, 2, true, 0.0, 4.0, 0.590, 0.834, 3.2e6, 0, 1},
-    {256, 256, 1, true, 0.0, 7.7, 1.034, 1.034, 2.2e6, 0, 1},
+    {128, 128, 2, true, 0.0, 4.0, 0.590, 0.834, 5.0e6, 0, 1},
+    {256, 256, 1, true, 0.0, 7.7, 1.034, 1.034, 5.0e6, 0, 1},
 };
 
 constexpr int64_t kInt8PartBytes = (int64_t)64 << 20;   // partial sums of ranges, at most
@@ -60,15 +60,25 @@ inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int6
     return f.launch + t;
 }
 
+// Workgroups of a form's launch, at most: blocks of one expert hold no places of another.
+inline int64_t int8_grid(int form, int64_t T, int64_t N, int64_t E, int splits) {
+    const Int8Cost &f = kInt8Costs[form];
+    const int64_t blocks = E == 0 ? cdiv(T, f.places) : T / f.places + std::min(E, T);
+    return blocks * cdiv(N, f.channels) * splits;
+}
+// (a launch has less than 2^32 threads; the persistent forms loop)
+constexpr int64_t kInt8MostWorkgroups = 0xFFFFFF;   // of 256 threads
+
 struct Int8Plan {
     int form, splits;
 };
 // `part_bytes`: room for partial sums
 inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64_t part_bytes) {
-    Int8Plan best{kInt8Few, 1};
+    Int8Plan best{kInt8Tile256, 1};
     double least = 1e300;
     for (int form = 0; form < kInt8Forms; ++form) {
         const Int8Cost &f = kInt8Costs[form];
+        if (!f.persistent && int8_grid(form, T, N, E, 1) > kInt8MostWorkgroups) continue;
         const bool cut = E == 0 && (form == kInt8Mid32 || form == kInt8Mid64);
         for (int s = 1; s <= (cut ? kInt8MaxSplits : 1); ++s) {
             // a range has two stages at least, and only grids of less than four rounds are cut
@@ -82,5 +92,18 @@ inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64
     }
     return best;
 }
+
+// Single tokens are quantized by every workgroup of the product for itself (mq_int8_few.hip): one launch instead of two.  A token more in a
+// workgroup costs 1.2 us, the launch saved 3 to 5: one token 4096 x 4096 10.7 -> 8.2 us, 4096 x 14336 21.9 -> 17.1, two experts 2304 x 9216 19.7
+// -> 14.5; three tokens are about level, four lose (4096 x 4096 10.9 against 11.9 us).
+constexpr int kInt8SinglePlaces = 4;                    // in all; an expert may have all of them
+constexpr int64_t kInt8SingleK = 16384, kInt8SingleBytes = 131072;   // of a token; of all tokens, in LDS
+inline bool int8_single(int64_t T, int64_t N, int64_t K, int64_t E) {
+    const int64_t used = E == 0 ? 1 : std::min(E, T);
+    return T <= kInt8SinglePlaces && T <= 3 * used && K <= kInt8SingleK && T * (K + 16) <= kInt8SingleBytes && cdiv(N, 16) * used <= kInt8MostWorkgroups;
+}
+// 32 channels to a workgroup instead of 16 where that leaves three workgroups to a compute unit: 28672 x 4096 27.6 -> 26.9 us, 14336 x 4096 16.5
+// -> 15.8; below, 4096 x 4096 8.2 -> 9.5.
+inline bool int8_single_wide(int64_t T, int64_t N, int64_t E) { return cdiv(N, 16) * (E == 0 ? 1 : std::min(E, T)) >= 768; }
 
 }  // namespace mq

@@ -1,4 +1,6 @@
 // The product in 8-bit integers for many tokens: tiles through LDS.
+#include <algorithm>
+
 #include "mq_int8.h"
 #include "mq_linear.h"
 
@@ -36,11 +38,22 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     typedef Int8Tile<RB, TB, WR, WC> T;
     typedef __attribute__((address_space(1))) void *global_ptr;
     constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL, NM = RB * TB;
-    static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0 && T::TN % 64 == 0 && T::TM % 64 == 0 && T::LDS <= 160 * 1024, "");
+    static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0 && T::TN % 64 == 0 && T::TM % 64 == 0 && T::LDS + 4 * (kMaxExperts + 1) <= 160 * 1024, "");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g4 = lane >> 4, l16 = lane & 15, wr = wave / WC, wc = wave % WC;
+
+    // The experts' bounds are kept in LDS, and only blocks that exist are counted: a workgroup's share of a bound on their number would leave
+    // XCDs idle.
+    const int32_t *bounds = reinterpret_cast<const int32_t *>(smem + T::LDS);
+    if (a.offsets) {
+        for (int e = threadIdx.x; e <= a.E; e += 64 * NW) reinterpret_cast<int32_t *>(smem + T::LDS)[e] = a.offsets[e];
+        __syncthreads();
+        find_block(a.T, a.E, 0, T::TM, [&](int e) { return bounds[e]; }, &tiles_m);
+        tiles_m = __builtin_amdgcn_readfirstlane(tiles_m);
+    }
     const int total = tiles_m * tiles_n;
+    if ((int)blockIdx.x >= total) return;
 
     struct Tile {
         Block b;
@@ -52,7 +65,9 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         const int width = GROUP * tiles_n;
         const int first_m = (int)(lid / width) * GROUP;
         const int gsz = min(tiles_m - first_m, GROUP);
-        return Tile{find_block(a, first_m + (int)(lid % width) % gsz, T::TM), (int)(lid % width) / gsz * T::TN};
+        const int block = first_m + (int)(lid % width) % gsz, n0 = (int)(lid % width) / gsz * T::TN;
+        if (!a.offsets) return Tile{Block{0, block * T::TM, min(T::TM, a.T - block * T::TM)}, n0};
+        return Tile{find_block(a.T, a.E, block, T::TM, [&](int e) { return bounds[e]; }), n0};
     };
 
     uint32_t coff[CL];
@@ -75,32 +90,39 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         else
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, k0 + col < a.K ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
     };
+    // The tokens whose rows and parameters this lane requests of a tile: found while the tile before is multiplied.
+    static_assert((T::TN + T::TM) / 64 == NW, "a wave fetches the parameters of 64 rows");
+    int tokens[XL], param_row;   // (as they stand in rows; nothing waits for them before begin)
+    auto look = [&](const Tile &t) {
+        const int lane = here(threadIdx.x & 63);
+        const int last = t.b.count - 1;
+        param_row = wave < T::TN / 64 ? min(t.n0 + wave * 64 + lane, a.N - 1) : t.b.place + min((wave - T::TN / 64) * 64 + lane, last);
+#pragma unroll
+        for (int i = 0; i < XL; ++i) tokens[i] = t.b.place + min(wave * 8 + (lane >> 3) + 8 * NW * i, last);
+        if (a.rows) {
+#pragma unroll
+            for (int i = 0; i < XL; ++i) tokens[i] = a.rows[tokens[i]];
+            if (wave >= T::TN / 64) param_row = a.rows[param_row];
+        }
+    };
     // A tile's parameters (set `set`) and its first two stages.
     auto begin = [&](const Tile &t, int set) {
-        const int lane = here(threadIdx.x & 63);
         rC = make_rsrc(a.codes + ((int64_t)t.b.expert * a.N + t.n0) * a.K, (uint64_t)(a.N - t.n0) * a.K);
-        const int64_t base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: launch_int8)
-        rX = make_rsrc(a.Xq + base * a.K, (uint64_t)(a.M - base) * a.K);
+        const int base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
+        rX = make_rsrc(a.Xq + (int64_t)base * a.K, (uint64_t)(a.M - base) * a.K);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) {
-            const int row = wave * 8 + (lane >> 3) + 8 * NW * i;
-            xoff[i] = (uint32_t)(token_of(a, t.b.place + min(row, t.b.count - 1)) - (int)base) * (uint32_t)a.K + (uint32_t)col;
+        for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)(min(max(tokens[i], 0), a.M - 1) - base) * (uint32_t)a.K + (uint32_t)col;
+        uint8_t *to = smem + T::PARAMS + set * T::PARAM_SET + wave * 512;
+        const void *one, *two;
+        if (wave < T::TN / 64) {
+            const int64_t n = (int64_t)t.b.expert * a.N + param_row;
+            one = a.alpha + n, two = a.zero + n;
+        } else {
+            const int m = min(max(param_row, 0), a.M - 1);
+            one = a.scale + m, two = a.sum + m;
         }
-        uint8_t *to = smem + T::PARAMS + set * T::PARAM_SET;
-        for (int i = wave; i < (T::TN + T::TM) / 64; i += NW) {   // 64 rows at a time
-            const bool channels = i < T::TN / 64;
-            const int row = (channels ? i : i - T::TN / 64) * 64 + lane;
-            const void *one, *two;
-            if (channels) {
-                const int64_t n = (int64_t)t.b.expert * a.N + min(t.n0 + row, a.N - 1);
-                one = a.alpha + n, two = a.zero + n;
-            } else {
-                const int m = token_of(a, t.b.place + min(row, t.b.count - 1));
-                one = a.scale + m, two = a.sum + m;
-            }
-            __builtin_amdgcn_global_load_lds((global_ptr)one, (lds_ptr)(to + i * 512), 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_ptr)two, (lds_ptr)(to + i * 512 + 256), 4, 0, 0);
-        }
+        __builtin_amdgcn_global_load_lds((global_ptr)one, (lds_ptr)to, 4, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)two, (lds_ptr)(to + 256), 4, 0, 0);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -203,40 +225,40 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
 
     int id = blockIdx.x, set = 0;
     Tile cur = tile_at(id);
-    if (cur.b.count > 0) begin(cur, set);
+    look(cur);
+    begin(cur, set);
     for (;;) {
         const int next_id = id + (int)gridDim.x;
-        Tile next = {};
-        if (next_id < total) next = tile_at(next_id);
-        if (cur.b.count > 0) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
+        for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
-            stage_barrier<LPS, 0>();
+            for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
+        stage_barrier<LPS, 0>();
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca[0] + rb * 2048));
+        for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca[0] + rb * 2048));
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa[0] + tb * 2048);
-            int k0 = 0, buf = 0;
-            auto stage = [&](auto inside_tag) {
-                half(inside_tag, std::integral_constant<int, 0>{}, k0, buf);
-                half(inside_tag, std::integral_constant<int, 1>{}, k0, buf);
-                k0 += 128;
-                buf = 1 - buf;
-            };
-            while (k0 + 384 <= a.K) stage(std::true_type{});
-            while (k0 < a.K) stage(std::false_type{});
-            mfma16_settle();
-            stage_barrier<0, 0>();   // the buffers are free
+        for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa[0] + tb * 2048);
+        Tile next = cur;
+        if (next_id < total) {
+            next = tile_at(next_id);
+            look(next);
         }
-        if (next.b.count > 0) begin(next, 1 - set);
-        if (cur.b.count > 0) {
-            if (a.gate)
-                finish(std::true_type{}, cur, set);
-            else
-                finish(std::false_type{}, cur, set);
-        }
+        int k0 = 0, buf = 0;
+        auto stage = [&](auto inside_tag) {
+            half(inside_tag, std::integral_constant<int, 0>{}, k0, buf);
+            half(inside_tag, std::integral_constant<int, 1>{}, k0, buf);
+            k0 += 128;
+            buf = 1 - buf;
+        };
+        while (k0 + 384 <= a.K) stage(std::true_type{});
+        while (k0 < a.K) stage(std::false_type{});
+        mfma16_settle();
+        stage_barrier<0, 0>();   // the buffers are free
+        if (next_id < total) begin(next, 1 - set);
+        if (a.gate)
+            finish(std::true_type{}, cur, set);
+        else
+            finish(std::false_type{}, cur, set);
         if (next_id >= total) break;
         id = next_id;
         cur = next;
@@ -252,12 +274,14 @@ namespace {
 template <bool R8, int RB, int TB, int WR, int WC, int WGS>
 mq_status launch_tile(const Int8Args &a, hipStream_t st) {
     typedef Int8Tile<RB, TB, WR, WC> T;
-    const int64_t tiles_n = cdiv(a.N, T::TN), tiles_m = block_bound(a.T, a.E, a.offsets != nullptr, T::TM);
-    if (tiles_n * tiles_m > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    const int64_t tiles_n = cdiv(a.N, T::TN), tiles = int8_grid(T::TM == 128 ? kInt8Tile128 : kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1);
+    const int64_t tiles_m = tiles / tiles_n;
+    if (tiles > 0x7FFFFF00) return MQ_ERR_SHAPE;
     constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, WGS>;
-    if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;
+    const int lds = T::LDS + (a.offsets ? (a.E + 1) * 4 : 0);
+    if (!allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
     const int64_t most = 256 * WGS;   // workgroups that fit the GPU
-    kernel<<<dim3((unsigned)(tiles_n * tiles_m < most ? tiles_n * tiles_m : most)), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n);
+    kernel<<<dim3((unsigned)std::min(tiles, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n);
     return launch_status();
 }
 
