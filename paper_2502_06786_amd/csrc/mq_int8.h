@@ -190,7 +190,7 @@ mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_
 mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
 // the same on bf16 tokens X [M, K], for up to kInt8SinglePlaces places and kInt8SingleK values a token
 mq_status launch_int8_single(const Int8Args &a, const uint16_t *X, hipStream_t st);
-// places: of a tile, 32 or 64; part: room for the partial sums of `splits` ranges of K
+// places: of a tile, 32, 64 or 96; part: room for the partial sums of `splits` ranges of K
 mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st);
 // places: of a tile, 128 or 256
 mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st);

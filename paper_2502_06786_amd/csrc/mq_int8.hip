@@ -102,6 +102,7 @@ mq_status launch_int8(const Int8Args &a, void *part, size_t part_bytes, hipStrea
         case kInt8Few: return launch_int8_few(a, st);
         case kInt8Mid32: return launch_int8_mid(a, 32, plan.splits, part, st);
         case kInt8Mid64: return launch_int8_mid(a, 64, plan.splits, part, st);
+        case kInt8Mid96: return launch_int8_mid(a, 96, plan.splits, part, st);
         case kInt8Tile128: return launch_int8_tiles(a, 128, st);
         default: return launch_int8_tiles(a, 256, st);
     }
@@ -167,6 +168,9 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
 
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
                                  float *scale, int32_t *sum, hipStream_t st) {
+    // With few rows a workgroup to each, which is done sooner: 16 tokens of 4096 values 4.6 -> 3.9 us; with many the fewest lanes that hold a row.
+    if (M <= 512 && K <= 4096) return launch_tokens<256, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
+    if (M <= 256 && K <= 16384) return launch_tokens<1024, 2, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
     if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
     if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
     return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);

@@ -154,10 +154,10 @@ namespace {
 template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
 mq_status launch_mid(const Int8Args &a, int splits, void *part, hipStream_t st) {
     typedef Int8Mid<RB, TB, WR, WC, NBUF> T;
-    const int64_t tiles_n = cdiv(a.N, T::TN), grid = int8_grid(T::TM == 32 ? kInt8Mid32 : kInt8Mid64, a.T, a.N, a.offsets ? a.E : 0, splits);
+    const int64_t tiles_n = cdiv(a.N, T::TN), grid = int8_grid(T::TM == 32 ? kInt8Mid32 : T::TM == 64 ? kInt8Mid64 : kInt8Mid96, a.T, a.N, a.offsets ? a.E : 0, splits);
     const int64_t tiles_m = grid / tiles_n / splits;
     if (grid > kInt8MostWorkgroups) return MQ_ERR_SHAPE;
-    static_assert(T::NW <= 4 && T::TN == 64 && (T::TM == 32 || T::TM == 64), "the forms of mq_int8_plan.h");
+    static_assert(T::NW <= 4 && T::TN == 64 && (T::TM == 32 || T::TM == 64 || T::TM == 96), "the forms of mq_int8_plan.h");
     constexpr auto kernel = int8_mid_kernel<R8, RB, TB, WR, WC, NBUF>;
     if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;
     const Int8Ranges s{static_cast<i32x4 *>(part), splits};
@@ -176,7 +176,9 @@ mq_status launch_mid_form(const Int8Args &a, int splits, void *part, hipStream_t
 }  // namespace
 
 mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st) {
-    return places == 32 ? launch_mid_form<1, 2, 4, 1, 4>(a, splits, part, st) : launch_mid_form<1, 4, 4, 1, 4>(a, splits, part, st);
+    return places == 32   ? launch_mid_form<1, 2, 4, 1, 4>(a, splits, part, st)
+           : places == 64 ? launch_mid_form<1, 4, 4, 1, 4>(a, splits, part, st)
+                          : launch_mid_form<1, 6, 4, 1, 4>(a, splits, part, st);
 }
 
 }  // namespace mq

@@ -11,27 +11,30 @@
 namespace mq {
 
 // FEW: 16 channels x 16 places, operands straight to registers, K over the waves (mq_int8_few.hip).
-// MID32, MID64: 64 channels x 32 or 64 places through LDS, K over workgroups where there are few tiles (mq_int8_mid.hip).
+// MID32, MID64, MID96: 64 channels x 32, 64 or 96 places through LDS, K over workgroups where there are few tiles (mq_int8_mid.hip).
 // TILE128, TILE256: persistent tiles of 128 x 128, two workgroups to a compute unit, and of 256 x 256 (mq_int8_tile.hip).
-enum Int8Form { kInt8Few, kInt8Mid32, kInt8Mid64, kInt8Tile128, kInt8Tile256, kInt8Forms };
+enum Int8Form { kInt8Few, kInt8Mid32, kInt8Mid64, kInt8Mid96, kInt8Tile128, kInt8Tile256, kInt8Forms };
 
 // What a form costs, in us.  A workgroup's stage of 128 k takes `alone` where it has a compute unit for itself and `full` where `per_cu` of
 // them share it; `end` is what a tile costs besides its stages, `launch` what a call does; codes and tokens arrive at `bytes_us` bytes in
-// a us at most, and ranges of K cost `join` and the traffic of their partial sums.  Fitted to 4372 times (12 layers from 6000 x 512 to
-// 28672 x 4096, 1 to 4096 tokens, 1 to 12 ranges; replayed from a graph, root mean square of the misfit 10 to 14 %).  The form that the rule
-// takes is 3 % slower than the best of these on average, 30 % at worst.
+// a us at most (the large tiles hold two stages: they wait for memory longer), and ranges of K cost `join` and the traffic of their
+// partial sums.  Fitted to 4500 times (12 layers from 6000 x 512 to 28672 x 4096, 1 to 4096 tokens, 1 to 12 ranges; replayed from a graph; root mean
+// square of the misfit 5 to 15 %).
 struct Int8Cost {
     int channels, places, per_cu;
     bool persistent;
     double launch, end, alone, full, bytes_us, join, join_bytes_us;
 };
 constexpr Int8Cost kInt8Costs[kInt8Forms] = {
-    {16, 16, 3, false, 1.82, 1.46, 0.091, 0.328, 5.2e6, 0, 1},
-    {64, 32, 3, false, 3.60, 0.25, 0.180, 0.449, 7.2e6, 1.64, 5.2e6},
-    {64, 64, 2, false, 3.87, 0.53, 0.245, 0.494, 6.4e6, 1.16, 5.9e6},
-    {128, 128, 2, true, 0.0, 4.0, 0.590, 0.834, 5.0e6, 0, 1},
-    {256, 256, 1, true, 0.0, 7.7, 1.034, 1.034, 5.0e6, 0, 1},
+    {16, 16, 3, false, 0.57, 2.48, 0.079, 0.216, 5.3e6, 0, 1},
+    {64, 32, 3, false, 2.43, 1.20, 0.183, 0.441, 5.3e6, 1.97, 7.7e6},
+    {64, 64, 2, false, 2.87, 1.29, 0.249, 0.487, 5.3e6, 1.53, 7.5e6},
+    {64, 96, 2, false, 3.42, 1.12, 0.337, 0.644, 5.3e6, 1.19, 7.5e6},
+    {128, 128, 2, true, 0.0, 4.0, 0.590, 0.834, 3.2e6, 0, 1},
+    {256, 256, 1, true, 0.0, 7.6, 1.032, 1.032, 2.25e6, 0, 1},
 };
+constexpr double kInt8TokensUs = 14e6;   // bytes of tokens that the FEW form's workgroups read from the L2s in a us
+constexpr double kInt8FindUs = 2.5;      // what finding its block costs a workgroup of a product by expert that has one block only
 
 constexpr int64_t kInt8PartBytes = (int64_t)64 << 20;   // partial sums of ranges, at most
 constexpr int kInt8MaxSplits = 16;
@@ -53,9 +56,10 @@ inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int6
         t = rounds * (stages * f.full + f.end) + (rest > 0 ? stages * (rest > 256.0 ? f.full : f.alone) + f.end : 0.0);
     } else {
         const double share = tiles / 256.0;
-        t = std::max(stages * f.alone, stages * f.full / f.per_cu * share) + f.end * std::max(1.0, share / f.per_cu);
+        t = std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
     }
     t = std::max(t, (used * (double)N * (double)K + (double)T * (double)K) / f.bytes_us);
+    if (f.places == 16) t += tiles * (double)std::min<int64_t>(T, 16) * (double)K / kInt8TokensUs;
     if (splits > 1) t += f.join + (double)int8_part_bytes(f, T, N, splits) * 2.0 / f.join_bytes_us;
     return f.launch + t;
 }
@@ -79,7 +83,7 @@ inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64
     for (int form = 0; form < kInt8Forms; ++form) {
         const Int8Cost &f = kInt8Costs[form];
         if (!f.persistent && int8_grid(form, T, N, E, 1) > kInt8MostWorkgroups) continue;
-        const bool cut = E == 0 && (form == kInt8Mid32 || form == kInt8Mid64);
+        const bool cut = E == 0 && form >= kInt8Mid32 && form <= kInt8Mid96;
         for (int s = 1; s <= (cut ? kInt8MaxSplits : 1); ++s) {
             // a range has two stages at least, and only grids of less than four rounds are cut
             if (s > 1 && (cdiv(K, 128) < 2 * s || cdiv(N, f.channels) * cdiv(T, f.places) > 1024 || int8_part_bytes(f, T, N, s) > part_bytes)) break;
