@@ -18,5 +18,6 @@ _BINDING_NAMES = {
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
-        return getattr(binding, name)
+        globals()[name] = getattr(binding, name)  # (found without this function from then on: it takes as long as a small call's checks)
+        return globals()[name]
     raise AttributeError(name)

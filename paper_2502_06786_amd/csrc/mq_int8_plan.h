@@ -44,6 +44,10 @@ inline int64_t int8_part_bytes(const Int8Cost &f, int64_t T, int64_t N, int spli
     return splits == 1 ? 0 : cdiv(N, f.channels) * cdiv(T, f.places) * f.channels * f.places * 4 * splits;
 }
 
+// A last round of at most this many 256-tiles is done in quarters of 128 x 128, up to two to a compute unit.
+constexpr int kInt8QuarterTiles = 128;
+constexpr double kInt8QuarterLaunchUs = 3.0;
+
 // T places of E experts (E = 0: a dense product), in blocks of a form.  How many an expert has is not known here: half a block more than
 // their share is what sizes that vary cost, on average.
 inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int64_t E, int splits) {
@@ -54,6 +58,10 @@ inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int6
     if (f.persistent) {
         const double wave = 256.0 * f.per_cu, rounds = (double)(int64_t)(tiles / wave), rest = tiles - rounds * wave;
         t = rounds * (stages * f.full + f.end) + (rest > 0 ? stages * (rest > 256.0 ? f.full : f.alone) + f.end : 0.0);
+        if (f.places == 256 && rounds > 0 && rest > 0 && rest <= kInt8QuarterTiles) {
+            const Int8Cost &q = kInt8Costs[kInt8Tile128];
+            t = rounds * (stages * f.full + f.end) + stages * (rest > 64.0 ? q.full : q.alone) + q.end + kInt8QuarterLaunchUs;
+        }
     } else {
         const double share = tiles / 256.0;
         t = std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);

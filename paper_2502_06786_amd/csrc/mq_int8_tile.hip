@@ -29,10 +29,15 @@ struct Int8Tile {
     static constexpr int LDS = OUT + NW * 16 * OS;
 };
 
+// What of a product a launch takes: all of its tiles; whole rounds of 256-tiles where the rest is done in quarters; that rest, in 128-tiles
+// (the others then find nothing to do).  How many tiles there are is known on the device only in products by expert, so both launches ask.
+enum Int8Part { kInt8All, kInt8Rounds, kInt8Quarters };
+__device__ __forceinline__ bool in_quarters(int total) { return total >= 256 && total % 256 != 0 && total % 256 <= kInt8QuarterTiles; }
+
 // Persistent: workgroup i takes tiles i, i + gridDim.x, ...; the first stages of a tile are requested before the outputs of the one
 // before are formed.
 template <bool R8, int RB, int TB, int WR, int WC, int WGS>
-__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Part part) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     typedef Int8Tile<RB, TB, WR, WC> T;
@@ -44,30 +49,46 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     const int g4 = lane >> 4, l16 = lane & 15, wr = wave / WC, wc = wave % WC;
 
     // The experts' bounds are kept in LDS, and only blocks that exist are counted: a workgroup's share of a bound on their number would leave
-    // XCDs idle.
+    // XCDs idle.  Tiles of `unit` places and channels are counted (tiles_m x tiles_n of them).
+    const int unit = part == kInt8Quarters ? 256 : T::TM;
     const int32_t *bounds = reinterpret_cast<const int32_t *>(smem + T::LDS);
     if (a.offsets) {
         for (int e = threadIdx.x; e <= a.E; e += 64 * NW) reinterpret_cast<int32_t *>(smem + T::LDS)[e] = a.offsets[e];
         __syncthreads();
-        find_block(a.T, a.E, 0, T::TM, [&](int e) { return bounds[e]; }, &tiles_m);
+        find_block(a.T, a.E, 0, unit, [&](int e) { return bounds[e]; }, &tiles_m);
         tiles_m = __builtin_amdgcn_readfirstlane(tiles_m);
     }
-    const int total = tiles_m * tiles_n;
-    if ((int)blockIdx.x >= total) return;
+    const int units = tiles_m * tiles_n, rest = units % 256;
+    const bool quartered = part != kInt8All && in_quarters(units);
+    const int total = part == kInt8Quarters ? (quartered ? rest * 4 : 0) : quartered ? units - rest : units;
 
     struct Tile {
         Block b;
         int n0;
     };
-    auto tile_at = [&](int id) {
-        const uint32_t lid = xcd_contiguous_id(id, total);
+    auto unit_at = [&](int lid) {
         constexpr int GROUP = 4;
         const int width = GROUP * tiles_n;
-        const int first_m = (int)(lid / width) * GROUP;
+        const int first_m = lid / width * GROUP;
         const int gsz = min(tiles_m - first_m, GROUP);
-        const int block = first_m + (int)(lid % width) % gsz, n0 = (int)(lid % width) / gsz * T::TN;
-        if (!a.offsets) return Tile{Block{0, block * T::TM, min(T::TM, a.T - block * T::TM)}, n0};
-        return Tile{find_block(a.T, a.E, block, T::TM, [&](int e) { return bounds[e]; }), n0};
+        const int block = first_m + lid % width % gsz, n0 = lid % width / gsz * unit;
+        if (!a.offsets) return Tile{Block{0, block * unit, min(unit, a.T - block * unit)}, n0};
+        return Tile{find_block(a.T, a.E, block, unit, [&](int e) { return bounds[e]; }), n0};
+    };
+    // the first tile from id on, in steps of the grid, that is not empty (quarters may be): id is left at it, or past the last
+    auto tile_from = [&](int &id) {
+        Tile t = {};
+        for (; id < total; id += (int)gridDim.x) {
+            const int lid = (int)xcd_contiguous_id(id, total);
+            if (part != kInt8Quarters) return unit_at(lid);
+            t = unit_at(units - rest + lid / 4);
+            const int down = (lid & 1) * T::TM;
+            t.b.place += down;
+            t.b.count = min(t.b.count - down, T::TM);
+            t.n0 += (lid >> 1 & 1) * T::TN;
+            if (t.b.count > 0 && t.n0 < a.N) break;
+        }
+        return t;
     };
 
     uint32_t coff[CL];
@@ -167,14 +188,16 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         });
     };
 
-    // the outputs of a tile, 16 places at a time through LDS that only this wave uses
+    // The outputs of a tile, 16 places at a time through LDS that only this wave uses; those of the next 16 are formed while the rows
+    // come back.
     auto finish = [&](auto gated_tag, const Tile &t, int set) {
         constexpr bool GATED = decltype(gated_tag)::value;
+        constexpr int shift = GATED ? 1 : 0, per = (2 * RB) >> shift, VEC = (16 * per + 63) / 64;   // per: chunks of 8 outputs in a row
         const int lane = here(threadIdx.x & 63), g4 = lane >> 4, l16 = lane & 15;
         const uint8_t *params = smem + T::PARAMS + set * T::PARAM_SET;
         uint8_t *out = smem + T::OUT + wave * 16 * T::OS;
-        constexpr int shift = GATED ? 1 : 0;
         const int n_out = a.N >> shift, first = (t.n0 + wr * 16 * RB) >> shift;
+        const int rows = t.b.count - wc * TB * 16;   // of this wave's places
         f32x4 ka[RB], kb[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -182,53 +205,74 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
             const uint8_t *at = params + (n >> 6) * 512 + (n & 63) * 4;
             channel_factors(*reinterpret_cast<const f32x4 *>(at), *reinterpret_cast<const f32x4 *>(at + 256), a.mult, a.offset, ka[rb], kb[rb]);
         }
+        float scale[TB], sum[TB];
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
-            const int row0 = (wc * TB + tb) * 16;
-            if (row0 >= t.b.count) break;
-            const uint8_t *at = params + T::TN * 8 + ((row0 + l16) >> 6) * 512 + ((row0 + l16) & 63) * 4;
-            const float scale = *reinterpret_cast<const float *>(at), sum = (float)*reinterpret_cast<const int32_t *>(at + 256);
+            const int row = (wc * TB + tb) * 16 + l16;
+            const uint8_t *at = params + T::TN * 8 + (row >> 6) * 512 + (row & 63) * 4;
+            scale[tb] = *reinterpret_cast<const float *>(at);
+            sum[tb] = (float)*reinterpret_cast<const int32_t *>(at + 256);
+        }
+        u32x2 o[RB];
+        auto form = [&](int tb) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 float y[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum, scale, ka[rb][e], kb[rb][e]);
+                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum[tb], scale[tb], ka[rb][e], kb[rb][e]);
                 if constexpr (GATED)
-                    *reinterpret_cast<uint32_t *>(out + l16 * T::OS + rb * 16 + 4 * g4) =
-                        pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
+                    o[rb][0] = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
                 else
-                    *reinterpret_cast<u32x2 *>(out + l16 * T::OS + rb * 32 + 8 * g4) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+                    o[rb] = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            constexpr int per = (2 * RB) >> shift;   // chunks of 8 outputs in a row
-            const int rows = min(16, t.b.count - row0);
-            uint16_t *y = a.Y + (int64_t)(t.b.place + row0) * n_out + first;
-            if (n_out % 8 == 0) {
+        };
+        auto put = [&]() {
 #pragma unroll
-                for (int i = 0; i < (16 * per + 63) / 64; ++i) {
-                    const int c = i * 64 + lane, row = c / per, ch = c % per;
-                    if (row < rows && first + ch * 8 < n_out)
-                        __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(out + row * T::OS + ch * 16),
-                                                    reinterpret_cast<u32x4 *>(y + (int64_t)row * n_out + ch * 8));
+            for (int rb = 0; rb < RB; ++rb) {
+                if constexpr (GATED)
+                    *reinterpret_cast<uint32_t *>(out + l16 * T::OS + rb * 16 + 4 * g4) = o[rb][0];
+                else
+                    *reinterpret_cast<u32x2 *>(out + l16 * T::OS + rb * 32 + 8 * g4) = o[rb];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        uint16_t *y = a.Y + (int64_t)(t.b.place + wc * TB * 16) * n_out + first;
+        form(0);
+        put();
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb, y += 16 * (int64_t)n_out) {
+            if (n_out % 8 == 0) {
+                u32x4 v[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = *reinterpret_cast<const u32x4 *>(out + (i * 64 + lane) / per % 16 * T::OS + (i * 64 + lane) % per * 16);
+                if (tb + 1 < TB) form(tb + 1);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const int row = (i * 64 + lane) / per, ch = (i * 64 + lane) % per;
+                    if (row < 16 && tb * 16 + row < rows && first + ch * 8 < n_out)
+                        __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4 *>(y + (int64_t)row * n_out + ch * 8));
                 }
             } else {
-                for (int c = lane; c < rows * per * 8; c += 64) {
+                for (int c = lane; c < min(16, rows - tb * 16) * per * 8; c += 64) {
                     const int row = c / (per * 8), ch = c % (per * 8);
                     if (first + ch < n_out) y[(int64_t)row * n_out + ch] = *reinterpret_cast<const uint16_t *>(out + row * T::OS + ch * 2);
                 }
+                if (tb + 1 < TB) form(tb + 1);
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+            if (tb + 1 < TB) put();
         }
     };
 
     int id = blockIdx.x, set = 0;
-    Tile cur = tile_at(id);
+    Tile cur = tile_from(id);
+    if (id >= total) return;
     look(cur);
     begin(cur, set);
     for (;;) {
-        const int next_id = id + (int)gridDim.x;
+        int next_id = id + (int)gridDim.x;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -238,11 +282,8 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca[0] + rb * 2048));
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa[0] + tb * 2048);
-        Tile next = cur;
-        if (next_id < total) {
-            next = tile_at(next_id);
-            look(next);
-        }
+        const Tile next = tile_from(next_id);
+        if (next_id < total) look(next);
         int k0 = 0, buf = 0;
         auto stage = [&](auto inside_tag) {
             half(inside_tag, std::integral_constant<int, 0>{}, k0, buf);
@@ -272,24 +313,34 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
 namespace {
 
 template <bool R8, int RB, int TB, int WR, int WC, int WGS>
-mq_status launch_tile(const Int8Args &a, hipStream_t st) {
+mq_status launch_tile(const Int8Args &a, Int8Part part, hipStream_t st) {
     typedef Int8Tile<RB, TB, WR, WC> T;
-    const int64_t tiles_n = cdiv(a.N, T::TN), tiles = int8_grid(T::TM == 128 ? kInt8Tile128 : kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1);
-    const int64_t tiles_m = tiles / tiles_n;
+    static_assert(T::TN == T::TM && (T::TM == 128 || T::TM == 256), "the forms of mq_int8_plan.h");
+    const int64_t unit = part == kInt8Quarters ? 256 : T::TM, tiles_n = cdiv(a.N, unit);
+    const int64_t tiles = int8_grid(unit == 128 ? kInt8Tile128 : kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
     if (tiles > 0x7FFFFF00) return MQ_ERR_SHAPE;
     constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, WGS>;
     const int lds = T::LDS + (a.offsets ? (a.E + 1) * 4 : 0);
     if (!allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
     const int64_t most = 256 * WGS;   // workgroups that fit the GPU
-    kernel<<<dim3((unsigned)std::min(tiles, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n);
+    kernel<<<dim3((unsigned)std::min(part == kInt8Quarters ? most : tiles, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n, part);
     return launch_status();
+}
+
+template <bool R8>
+mq_status launch_tiles(const Int8Args &a, int places, hipStream_t st) {
+    if (places == 128) return launch_tile<R8, 4, 4, 2, 2, 2>(a, kInt8All, st);
+    // (with experts the number of tiles is a bound: the launch for the rest may find nothing to do)
+    const int64_t tiles = int8_grid(kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1);
+    if (tiles < 256 || (!a.offsets && (tiles % 256 == 0 || tiles % 256 > kInt8QuarterTiles))) return launch_tile<R8, 4, 8, 4, 2, 1>(a, kInt8All, st);
+    const mq_status s = launch_tile<R8, 4, 8, 4, 2, 1>(a, kInt8Rounds, st);
+    return s != MQ_OK ? s : launch_tile<R8, 4, 4, 2, 2, 2>(a, kInt8Quarters, st);
 }
 
 }  // namespace
 
 mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st) {
-    if (places == 128) return a.offset != 0.f ? launch_tile<true, 4, 4, 2, 2, 2>(a, st) : launch_tile<false, 4, 4, 2, 2, 2>(a, st);
-    return a.offset != 0.f ? launch_tile<true, 4, 8, 4, 2, 1>(a, st) : launch_tile<false, 4, 8, 4, 2, 1>(a, st);
+    return a.offset != 0.f ? launch_tiles<true>(a, places, st) : launch_tiles<false>(a, places, st);
 }
 
 }  // namespace mq
