@@ -544,8 +544,8 @@ mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, con
  *
  * mq_experts_combine:  out[m,n] = bf16(sum_j weight[m,j] * Y[place[m,j], n])   over the choices with 0 <= place[m,j] < T, in their
  * order, in fp32; a token without any gets zeros.
- *   Y [T, N] bf16;  place [M, top] int32;  weight [M, top] fp32;  out [M, N] bf16 out;  M N below 2^35 (N a multiple of 8, otherwise
- *   below 2^32)
+ *   Y [T, N] bf16;  place [M, top] int32;  weight [M, top] fp32;  out [M, N] bf16 out
+ * M * ceil(N / 1024) (N not a multiple of 8: M * ceil(N / 128)) below 2^25.
  */
 mq_status mq_experts_route(const int32_t *ids, int64_t M, int64_t top, int64_t E, int32_t *offsets, int32_t *rows, int32_t *place,
                            void *ws, size_t ws_bytes, void *hip_stream);

@@ -29,7 +29,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
     int32_t *total = base + padded;                                              // [padded]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * kRouteChunk;
 
-    for (int i = threadIdx.x; i < GROUPS * padded / 2; i += kRouteThreads) reinterpret_cast<uint32_t *>(smem)[i] = 0;
+    const int groups = min(GROUPS, (a.n - first + 63) / 64);   // that there are choices for
+    for (int i = threadIdx.x; i < (groups * padded + 1) / 2; i += kRouteThreads) reinterpret_cast<uint32_t *>(smem)[i] = 0;
     __syncthreads();
     int bucket[kRouteSteps], rank[kRouteSteps];
 #pragma unroll
@@ -55,10 +56,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
     __syncthreads();
     for (int b = threadIdx.x; b < buckets; b += kRouteThreads) {
         int sum = 0;
-        for (int g = 0; g < GROUPS; ++g) {
-            const int c = count[g * padded + b];
-            count[g * padded + b] = (uint16_t)sum;
-            sum += c;
+        for (int g0 = 0; g0 < groups; g0 += 8) {   // eight counts on their way at a time
+            int c[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) c[g] = g0 + g < groups ? count[(g0 + g) * padded + b] : 0;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                if (g0 + g < groups) count[(g0 + g) * padded + b] = (uint16_t)sum;
+                sum += c[g];
+            }
         }
         if constexpr (PLACES) {
             int before = 0, all = sum;
@@ -115,35 +121,55 @@ struct CombineArgs {
     const int32_t *place;
     const float *weight;
     uint16_t *out;
-    int64_t M, N;
+    uint32_t N;
     int top, T;
 };
 
-template <int V>  // values per thread: 8 where rows are whole 16-byte chunks, otherwise 1
-__global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
-    const int64_t chunks = a.N / V, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.M * chunks) return;
-    const int64_t m = i / chunks, n = (i - m * chunks) * V;
+// Workgroup = up to 128 chunks of one token's row: the places and weights are the same for all its lanes.  V: values per thread, 8 where rows
+// are whole 16-byte chunks, otherwise 1.
+template <int V>
+__global__ __launch_bounds__(128) void combine_kernel(CombineArgs a, uint32_t parts) {
+    const uint32_t m = blockIdx.x / parts, n = ((blockIdx.x - m * parts) * 128 + threadIdx.x) * V;
+    if (n >= a.N) return;
+    const int32_t *place = a.place + (int64_t)m * a.top;
+    const float *weight = a.weight + (int64_t)m * a.top;
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.f;
-    for (int j = 0; j < a.top; ++j) {
-        const int p = a.place[m * a.top + j];
-        if (p < 0 || p >= a.T) continue;
-        const float w = a.weight[m * a.top + j];
-        const uint16_t *y = a.Y + (int64_t)p * a.N + n;
-        if constexpr (V == 8) {
-            const u32x4 d = *reinterpret_cast<const u32x4 *>(y);
+    for (int j0 = 0; j0 < a.top; j0 += 4) {   // four rows on their way at a time
+        int p[4];
+        float w[4];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                sum[2 * v] = __builtin_fmaf(w, bf16_lo(d[v]), sum[2 * v]);
-                sum[2 * v + 1] = __builtin_fmaf(w, bf16_hi(d[v]), sum[2 * v + 1]);
+        for (int j = 0; j < 4; ++j) {
+            p[j] = j0 + j < a.top ? place[j0 + j] : -1;
+            w[j] = j0 + j < a.top ? weight[j0 + j] : 0.f;
+        }
+        u32x4 d[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            d[j] = u32x4{0u, 0u, 0u, 0u};
+            if (p[j] < 0 || p[j] >= a.T) continue;
+            const uint16_t *y = a.Y + (int64_t)p[j] * a.N + n;
+            if constexpr (V == 8)
+                d[j] = *reinterpret_cast<const u32x4 *>(y);
+            else
+                d[j][0] = *y;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (p[j] < 0 || p[j] >= a.T) continue;   // (its weight may be anything)
+            if constexpr (V == 8) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    sum[2 * v] = __builtin_fmaf(w[j], bf16_lo(d[j][v]), sum[2 * v]);
+                    sum[2 * v + 1] = __builtin_fmaf(w[j], bf16_hi(d[j][v]), sum[2 * v + 1]);
+                }
+            } else {
+                sum[0] = __builtin_fmaf(w[j], bf16_bits_to_float(d[j][0]), sum[0]);
             }
-        } else {
-            sum[0] = __builtin_fmaf(w, bf16_bits_to_float(*y), sum[0]);
         }
     }
-    uint16_t *out = a.out + m * a.N + n;
+    uint16_t *out = a.out + (int64_t)m * a.N + n;
     if constexpr (V == 8)
         *reinterpret_cast<u32x4 *>(out) = u32x4{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]), pack_bf16x2(sum[4], sum[5]),
                                                 pack_bf16x2(sum[6], sum[7])};
@@ -199,14 +225,14 @@ extern "C" mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place,
     if (M == 0 || N == 0) return MQ_OK;
     if ((T > 0 && !Y) || !place || !weight || !out) return MQ_ERR_NULL;
     if (!aligned16(Y) || !aligned16(place) || !aligned16(weight) || !aligned16(out)) return MQ_ERR_ALIGN;
-    const CombineArgs a{Y, place, weight, out, M, N, (int)top, (int)T};
+    const CombineArgs a{Y, place, weight, out, (uint32_t)N, (int)top, (int)T};
     const int V = N % 8 == 0 ? 8 : 1;
-    const int64_t blocks = cdiv(M * (N / V), 256);
-    if (blocks > 0xFFFFFF) return MQ_ERR_SHAPE;   // (a launch has less than 2^32 threads)
+    const int64_t parts = cdiv(N / V, 128), blocks = M * parts;
+    if (blocks > 0x1FFFFFF) return MQ_ERR_SHAPE;   // (a launch has less than 2^32 threads)
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (V == 8)
-        combine_kernel<8><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
+        combine_kernel<8><<<dim3((unsigned)blocks), dim3(128), 0, st>>>(a, (uint32_t)parts);
     else
-        combine_kernel<1><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
+        combine_kernel<1><<<dim3((unsigned)blocks), dim3(128), 0, st>>>(a, (uint32_t)parts);
     return launch_status();
 }
