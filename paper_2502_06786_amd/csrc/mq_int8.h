@@ -129,9 +129,10 @@ __device__ __forceinline__ Block find_block(int T, int E, int block, int BM, Bou
         }
         const uint64_t past = __ballot(upto > block);
         if (past && found.count == 0) {
-            const int at = __builtin_ctzll(past);
-            const int first = __builtin_amdgcn_readlane(upto - mine, at), place = __builtin_amdgcn_readlane(lo, at) + (block - first) * BM;
-            found = Block{e0 + at, place, min(BM, __builtin_amdgcn_readlane(hi, at) - place)};
+            const int at = __builtin_ctzll(past), nth = block - __builtin_amdgcn_readlane(upto - mine, at);
+            const int place = __builtin_amdgcn_readlane(lo, at) + nth * BM;
+            // (bounds that descend may wrap the sums: nothing is found then)
+            if ((uint32_t)nth < (uint32_t)__builtin_amdgcn_readlane(mine, at)) found = Block{e0 + at, place, min(BM, __builtin_amdgcn_readlane(hi, at) - place)};
             if (!blocks) return found;
         }
         before = __builtin_amdgcn_readlane(upto, 63);

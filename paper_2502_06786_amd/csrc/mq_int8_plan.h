@@ -35,7 +35,7 @@ constexpr Int8Cost kInt8Costs[kInt8Forms] = {
 };
 constexpr double kInt8TokensUs = 14e6;   // bytes of tokens that the FEW form's workgroups read from the L2s in a us
 // Products by expert (fitted to 75 times of 8 to 64 experts with 8 to 125 tokens each, the form taken 2 % slower than the best of five on average,
-// 14 % at worst): finding its block costs a workgroup that has one block only `kInt8FindUs`; codes that few tiles share come late, which the
+// 14 % at worst): finding its block costs a workgroup `kInt8FindUs` (a persistent one keeps the experts' bounds); codes that few tiles share come late, which the
 // small tiles' stages feel (`kInt8ExpertStage` times as long) and the large ones, which are more at a time, less than with one matrix
 // (`kInt8ExpertBytes` times the bytes).
 constexpr double kInt8FindUs = 2.5, kInt8ExpertStage = 1.6, kInt8ExpertBytes = 1.5;
@@ -71,6 +71,7 @@ inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int6
         t = (E ? kInt8ExpertStage : 1.0) * std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
     }
     t = std::max(t, (used * (double)N * (double)K + (double)T * (double)K) / (f.bytes_us * (E && f.persistent ? kInt8ExpertBytes : 1.0)));
+    if (E && f.persistent) t += kInt8FindUs;
     if (f.places == 16) t += tiles * (double)std::min<int64_t>(T, 16) * (double)K / kInt8TokensUs;
     if (splits > 1) t += f.join + (double)int8_part_bytes(f, T, N, splits) * 2.0 / f.join_bytes_us;
     return f.launch + t;

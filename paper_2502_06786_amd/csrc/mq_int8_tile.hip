@@ -55,8 +55,9 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     if (a.offsets) {
         for (int e = threadIdx.x; e <= a.E; e += 64 * NW) reinterpret_cast<int32_t *>(smem + T::LDS)[e] = a.offsets[e];
         __syncthreads();
-        find_block(a.T, a.E, 0, unit, [&](int e) { return bounds[e]; }, &tiles_m);
-        tiles_m = __builtin_amdgcn_readfirstlane(tiles_m);
+        int blocks;
+        find_block(a.T, a.E, 0, unit, [&](int e) { return bounds[e]; }, &blocks);
+        tiles_m = min(max(__builtin_amdgcn_readfirstlane(blocks), 0), tiles_m);
     }
     const int units = tiles_m * tiles_n, rest = units % 256;
     const bool quartered = part != kInt8All && in_quarters(units);
@@ -80,12 +81,13 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         Tile t = {};
         for (; id < total; id += (int)gridDim.x) {
             const int lid = (int)xcd_contiguous_id(id, total);
-            if (part != kInt8Quarters) return unit_at(lid);
-            t = unit_at(units - rest + lid / 4);
-            const int down = (lid & 1) * T::TM;
-            t.b.place += down;
-            t.b.count = min(t.b.count - down, T::TM);
-            t.n0 += (lid >> 1 & 1) * T::TN;
+            t = unit_at(part == kInt8Quarters ? units - rest + lid / 4 : lid);
+            if (part == kInt8Quarters) {
+                const int down = (lid & 1) * T::TM;
+                t.b.place += down;
+                t.b.count = min(t.b.count - down, T::TM);
+                t.n0 += (lid >> 1 & 1) * T::TN;
+            }
             if (t.b.count > 0 && t.n0 < a.N) break;
         }
         return t;

@@ -24,18 +24,28 @@ def act(g, gate):
         return g / (1.0 + np.exp(-arg)), np.abs(arg)
 
 
+def code_offset(r):
+    """What is taken off a code before the product: the bar below is that of sums of centred codes."""
+    return 128.0 if r == 8 else 0.0
+
+
 def layer(codes_x, scale, codes, alpha, zero, r, gate=None):
-    """(outputs in 64 bits, bar): |got - outputs| <= bar element by element.
+    """(outputs in 64 bits, bar): |got - outputs| <= bar element by element."""
+    cx = codes_x.astype(np.float64)
+    return outputs(cx @ (codes.astype(np.float64) - code_offset(r)).T, cx.sum(axis=1), scale, alpha, zero, r, gate)
+
+
+def outputs(dot, sums, scale, alpha, zero, r, gate=None):
+    """layer() from dot [M, N] = sum over k of token code times (code - code_offset) and sums [M] of the tokens' codes.
 
     The fp32 steps after the exact sums: dot, sum, zero - offset and five operations on them, each off by 2^-24 of terms that are
-    not larger than 2^(8-r) |dot| and (|zero| + 128) |sum|: 8 of those at most.  Then one rounding to bf16 (8 significant bits: half a spacing is at most 2^-8 of the value).
-    With a gate, the errors of both outputs pass through a * u (|act'| <= 1.13), and the exponential adds (4 + 2 |argument|) 2^-22
-    of the value: its argument is off by a few 2^-24 of itself, and an absolute error of the argument is a relative one of the result."""
-    cx, c = codes_x.astype(np.float64), codes.astype(np.float64)
-    mult = float(1 << (8 - r))
-    off = 128.0 if r == 8 else 0.0
-    dot, sums = cx @ (c - off).T, cx.sum(axis=1, keepdims=True)
+    not larger than 2^(8-r) |dot| and (|zero| + 128) |sum|: 8 of those at most.  Then one rounding to bf16 (8 significant bits: half a
+    spacing is at most 2^-8 of the value).  With a gate, the errors of both outputs pass through a * u (|act'| <= 1.13), and the
+    exponential adds (4 + 2 |argument|) 2^-22 of the value: its argument is off by a few 2^-24 of itself, and an absolute error of the
+    argument is a relative one of the result."""
+    mult, off = float(1 << (8 - r)), code_offset(r)
     a, z, s = alpha.astype(np.float64), zero.astype(np.float64), scale.astype(np.float64)[:, None]
+    sums = np.asarray(sums, np.float64)[:, None]
     y = a * (mult * dot - (z - off) * sums) * s
     err = 8 * 2.0 ** -24 * np.abs(a * s) * (mult * np.abs(dot) + (np.abs(z) + 128.0) * np.abs(sums)) + 2.0 ** -140
     if gate is None:
