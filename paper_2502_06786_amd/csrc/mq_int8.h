@@ -186,6 +186,45 @@ __device__ __forceinline__ void load_factors(const Int8Args &a, int expert, int 
     channel_factors(al, ze, a.mult, a.offset, ka, kb);
 }
 
+// ---- ranges of K ------------------------------------------------------------------------------------------
+struct Int8Ranges {
+    i32x4 *part;  // [split][tile][wave, rb, tb][lane]
+    int splits;
+};
+
+// Adds the ranges (whole numbers: in any order) and finishes the outputs: a wave for each block of 16 channels x 16 places of tiles of
+// WR x WC waves with RB x TB blocks each.  Dense products only.
+template <int RB, int TB, int WR, int WC>
+__global__ __launch_bounds__(256) void int8_join_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
+    constexpr int NW = WR * WC, BLOCKS = NW * RB * TB;
+    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, id = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int tile = id / BLOCKS, wave = id % BLOCKS / (RB * TB), rb = id / TB % RB, tb = id % TB, wr = wave / WC, wc = wave % WC;
+    const int tiles = tiles_m * tiles_n;
+    if (tile >= tiles) return;
+    const int row = tile % tiles_m * (16 * TB * WC) + (wc * TB + tb) * 16 + l16, n = tile / tiles_m * (16 * RB * WR) + (wr * RB + rb) * 16 + 4 * g4;
+    if (row >= a.T || n >= a.N) return;
+    const i32x4 *from = s.part + (int64_t)id * 64 + lane;
+    const int64_t step = (int64_t)tiles * BLOCKS * 64;
+    f32x4 ka, kb;
+    load_factors(a, 0, n, ka, kb);
+    const float scale = a.scale[row], sum = (float)a.sum[row];
+    i32x4 dot = {0, 0, 0, 0};
+    for (int i = 0; i < s.splits; i += 4) {   // four loads in flight
+        i32x4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = i + j < s.splits ? from[(i + j) * step] : i32x4{0, 0, 0, 0};
+        dot += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    store_four(a, row, n, dot, scale, sum, ka, kb);
+}
+
+template <int RB, int TB, int WR, int WC>
+mq_status launch_int8_join(const Int8Args &a, const Int8Ranges &s, hipStream_t st) {
+    const int64_t tiles_n = cdiv(a.N, 16 * RB * WR), tiles_m = cdiv(a.T, 16 * TB * WC);
+    int8_join_kernel<RB, TB, WR, WC><<<dim3((unsigned)cdiv(tiles_n * tiles_m * WR * WC * RB * TB, 4)), dim3(256), 0, st>>>(a, (int)tiles_m, (int)tiles_n, s);
+    return launch_status();
+}
+
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
                                  float *scale, int32_t *sum, hipStream_t st);
 mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
@@ -193,7 +232,7 @@ mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
 mq_status launch_int8_single(const Int8Args &a, const uint16_t *X, hipStream_t st);
 // places: of a tile, 32, 64 or 96; part: room for the partial sums of `splits` ranges of K
 mq_status launch_int8_mid(const Int8Args &a, int places, int splits, void *part, hipStream_t st);
-// places: of a tile, 128 or 256
-mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st);
+// form: kInt8Deep128 (which may be cut), kInt8Tile128 or kInt8Tile256
+mq_status launch_int8_tiles(const Int8Args &a, Int8Form form, int splits, void *part, hipStream_t st);
 
 }  // namespace mq

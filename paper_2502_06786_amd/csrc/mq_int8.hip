@@ -103,8 +103,7 @@ mq_status launch_int8(const Int8Args &a, void *part, size_t part_bytes, hipStrea
         case kInt8Mid32: return launch_int8_mid(a, 32, plan.splits, part, st);
         case kInt8Mid64: return launch_int8_mid(a, 64, plan.splits, part, st);
         case kInt8Mid96: return launch_int8_mid(a, 96, plan.splits, part, st);
-        case kInt8Tile128: return launch_int8_tiles(a, 128, st);
-        default: return launch_int8_tiles(a, 256, st);
+        default: return launch_int8_tiles(a, (Int8Form)plan.form, plan.splits, part, st);
     }
 }
 

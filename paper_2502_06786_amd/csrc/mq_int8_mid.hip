@@ -12,11 +12,6 @@ struct Int8Mid {
     static constexpr int STAGE = (TN + TM) * 128, LDS = NBUF * STAGE;
 };
 
-struct Int8Ranges {
-    i32x4 *part;  // [split][tile][wave, rb, tb][lane]
-    int splits;
-};
-
 template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
 __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
@@ -123,32 +118,6 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
 #endif
 }
 
-// Adds the ranges (whole numbers: in any order) and finishes the outputs: a wave for each block of 16 channels x 16 places.  Dense products
-// only.
-template <int RB, int TB, int WR, int WC>
-__global__ __launch_bounds__(256) void int8_mid_finish_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
-    constexpr int NW = WR * WC, BLOCKS = NW * RB * TB;
-    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, id = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int tile = id / BLOCKS, wave = id % BLOCKS / (RB * TB), rb = id / TB % RB, tb = id % TB, wr = wave / WC, wc = wave % WC;
-    const int tiles = tiles_m * tiles_n;
-    if (tile >= tiles) return;
-    const int row = tile % tiles_m * (16 * TB * WC) + (wc * TB + tb) * 16 + l16, n = tile / tiles_m * (16 * RB * WR) + (wr * RB + rb) * 16 + 4 * g4;
-    if (row >= a.T || n >= a.N) return;
-    const i32x4 *from = s.part + (int64_t)id * 64 + lane;
-    const int64_t step = (int64_t)tiles * BLOCKS * 64;
-    f32x4 ka, kb;
-    load_factors(a, 0, n, ka, kb);
-    const float scale = a.scale[row], sum = (float)a.sum[row];
-    i32x4 dot = {0, 0, 0, 0};
-    for (int i = 0; i < s.splits; i += 4) {   // four loads in flight
-        i32x4 v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = i + j < s.splits ? from[(i + j) * step] : i32x4{0, 0, 0, 0};
-        dot += (v[0] + v[1]) + (v[2] + v[3]);
-    }
-    store_four(a, row, n, dot, scale, sum, ka, kb);
-}
-
 namespace {
 
 template <bool R8, int RB, int TB, int WR, int WC, int NBUF>
@@ -163,9 +132,7 @@ mq_status launch_mid(const Int8Args &a, int splits, void *part, hipStream_t st) 
     const Int8Ranges s{static_cast<i32x4 *>(part), splits};
     kernel<<<dim3((unsigned)grid), dim3(64 * T::NW), T::LDS, st>>>(a, (int)tiles_m, (int)tiles_n, s);
     const mq_status status = launch_status();
-    if (status != MQ_OK || splits == 1) return status;
-    int8_mid_finish_kernel<RB, TB, WR, WC><<<dim3((unsigned)cdiv(tiles_n * tiles_m * T::NW * RB * TB, 4)), dim3(256), 0, st>>>(a, (int)tiles_m, (int)tiles_n, s);
-    return launch_status();
+    return status != MQ_OK || splits == 1 ? status : launch_int8_join<RB, TB, WR, WC>(a, s, st);
 }
 
 template <int RB, int TB, int WR, int WC, int NBUF>

@@ -12,32 +12,35 @@ namespace mq {
 
 // FEW: 16 channels x 16 places, operands straight to registers, K over the waves (mq_int8_few.hip).
 // MID32, MID64, MID96: 64 channels x 32, 64 or 96 places through LDS, K over workgroups where there are few tiles (mq_int8_mid.hip).
-// TILE128, TILE256: persistent tiles of 128 x 128, two workgroups to a compute unit, and of 256 x 256 (mq_int8_tile.hip).
-enum Int8Form { kInt8Few, kInt8Mid32, kInt8Mid64, kInt8Mid96, kInt8Tile128, kInt8Tile256, kInt8Forms };
+// DEEP128, TILE128, TILE256: tiles that are looped over (mq_int8_tile.hip): of 128 x 128 with four stages in LDS, one workgroup to a compute unit,
+// K over workgroups where there are few tiles; of 128 x 128, two workgroups to a compute unit; of 256 x 256.
+enum Int8Form { kInt8Few, kInt8Mid32, kInt8Mid64, kInt8Mid96, kInt8Deep128, kInt8Tile128, kInt8Tile256, kInt8Forms };
 
 // What a form costs, in us.  A workgroup's stage of 128 k takes `alone` where it has a compute unit for itself and `full` where `per_cu` of
 // them share it; `end` is what a tile costs besides its stages, `launch` what a call does; codes and tokens arrive at `bytes_us` bytes in
 // a us at most (the large tiles hold two stages: they wait for memory longer), and ranges of K cost `join` and the traffic of their
-// partial sums.  Fitted to 4500 times (12 layers from 6000 x 512 to 28672 x 4096, 1 to 4096 tokens, 1 to 12 ranges; replayed from a graph; root mean
-// square of the misfit 5 to 15 %).
+// partial sums.  Fitted to 5600 times (13 layers from 6000 x 512 to 28672 x 4096, 1 to 4096 tokens, 1 to 16 ranges; replayed from a graph; root mean
+// square of the misfit 5 to 12 %): of the forms and ranges timed at 259 sizes, the one that the rule takes is 3 % slower than the best on
+// average, 25 % at worst.
 struct Int8Cost {
     int channels, places, per_cu;
-    bool persistent;
+    bool looped;
     double launch, end, alone, full, bytes_us, join, join_bytes_us;
 };
 constexpr Int8Cost kInt8Costs[kInt8Forms] = {
     {16, 16, 3, false, 0.57, 2.48, 0.079, 0.216, 5.3e6, 0, 1},
-    {64, 32, 3, false, 2.43, 1.20, 0.183, 0.441, 5.3e6, 1.97, 7.7e6},
-    {64, 64, 2, false, 2.87, 1.29, 0.249, 0.487, 5.3e6, 1.53, 7.5e6},
-    {64, 96, 2, false, 3.42, 1.12, 0.337, 0.644, 5.3e6, 1.19, 7.5e6},
-    {128, 128, 2, true, 0.0, 4.0, 0.590, 0.834, 3.2e6, 0, 1},
-    {256, 256, 1, true, 0.0, 7.6, 1.032, 1.032, 2.25e6, 0, 1},
+    {64, 32, 3, false, 2.38, 1.29, 0.182, 0.438, 5.3e6, 2.01, 7.8e6},
+    {64, 64, 2, false, 2.92, 1.23, 0.251, 0.484, 5.3e6, 1.50, 7.3e6},
+    {64, 96, 2, false, 3.41, 1.37, 0.335, 0.614, 5.2e6, 1.21, 7.1e6},
+    {128, 128, 1, true, 2.76, 2.94, 0.319, 0.487, 5.3e6, 1.98, 6.5e6},
+    {128, 128, 2, true, 0.0, 3.94, 0.601, 0.823, 3.2e6, 0, 1},
+    {256, 256, 1, true, 0.0, 7.57, 1.033, 1.033, 2.25e6, 0, 1},
 };
 constexpr double kInt8TokensUs = 14e6;   // bytes of tokens that the FEW form's workgroups read from the L2s in a us
-// Products by expert (fitted to 75 times of 8 to 64 experts with 8 to 125 tokens each, the form taken 2 % slower than the best of five on average,
-// 14 % at worst): finding its block costs a workgroup `kInt8FindUs` (a persistent one keeps the experts' bounds); codes that few tiles share come late, which the
-// small tiles' stages feel (`kInt8ExpertStage` times as long) and the large ones, which are more at a time, less than with one matrix
-// (`kInt8ExpertBytes` times the bytes).
+// Products by expert (105 times of 8 to 64 experts with 8 to 125 tokens each): finding its block costs a workgroup `kInt8FindUs` (one that loops
+// over tiles keeps the experts' bounds); codes that few tiles share come late, which a stage feels (`kInt8ExpertStage` times as long), while
+// the tiles with two stages get more bytes in a us than from one matrix (`kInt8ExpertBytes` times).  The form taken is 2 % slower than the best on
+// average, 12 % at worst.
 constexpr double kInt8FindUs = 2.5, kInt8ExpertStage = 1.6, kInt8ExpertBytes = 1.5;
 
 constexpr int64_t kInt8PartBytes = (int64_t)64 << 20;   // partial sums of ranges, at most
@@ -49,30 +52,34 @@ inline int64_t int8_part_bytes(const Int8Cost &f, int64_t T, int64_t N, int spli
 }
 
 // A last round of at most this many 256-tiles is done in quarters of 128 x 128, up to two to a compute unit.
-constexpr int kInt8QuarterTiles = 128;
+// (by the form with four stages where there is one to a compute unit at most)
+constexpr int kInt8QuarterTiles = 128, kInt8DeepQuarterTiles = 64;
 constexpr double kInt8QuarterLaunchUs = 3.0;
 
 // T places of E experts (E = 0: a dense product), in blocks of a form.  How many an expert has is not known here: half a block more than
 // their share is what sizes that vary cost, on average.
-inline double int8_cost(const Int8Cost &f, int64_t T, int64_t N, int64_t K, int64_t E, int splits) {
+inline double int8_cost(int form, int64_t T, int64_t N, int64_t K, int64_t E, int splits) {
+    const Int8Cost &f = kInt8Costs[form];
     const double used = E == 0 ? 1.0 : (double)std::min(E, T);
     const double blocks = E == 0 ? (double)cdiv(T, f.places) : used * std::max(1.0, (double)T / used / f.places + 0.5);
-    const double tiles = blocks * (double)cdiv(N, f.channels) * splits, stages = (double)cdiv(K, 128) / splits;
-    double t;
-    if (f.persistent) {
+    const double tiles = blocks * (double)cdiv(N, f.channels) * splits, slow = E ? kInt8ExpertStage : 1.0, stages = slow * (double)cdiv(K, 128) / splits;
+    double t, rate = f.bytes_us;
+    if (f.looped) {
         const double wave = 256.0 * f.per_cu, rounds = (double)(int64_t)(tiles / wave), rest = tiles - rounds * wave;
-        t = rounds * (stages * f.full + f.end) + (rest > 0 ? stages * (rest > 256.0 ? f.full : f.alone) + f.end : 0.0);
-        if (f.places == 256 && rounds > 0 && rest > 0 && rest <= kInt8QuarterTiles) {
-            const Int8Cost &q = kInt8Costs[kInt8Tile128];
-            t = rounds * (stages * f.full + f.end) + stages * (rest > 64.0 ? q.full : q.alone) + q.end + kInt8QuarterLaunchUs;
-        }
+        // the last round: compute units that share their L2 with fewer others wait less
+        double last = rest > 0 ? stages * (rest > 256.0 ? f.full : f.alone) + f.end : 0.0;
+        if (form == kInt8Deep128 && rest > 0) last = stages * std::max(f.alone, f.full * rest / 256.0) + f.end;
+        if (form == kInt8Tile256 && rounds > 0 && rest > 0 && rest <= kInt8QuarterTiles)
+            last = rest <= kInt8DeepQuarterTiles ? stages * kInt8Costs[kInt8Deep128].full + kInt8Costs[kInt8Deep128].end + kInt8QuarterLaunchUs
+                                                 : stages * kInt8Costs[kInt8Tile128].full + kInt8Costs[kInt8Tile128].end + kInt8QuarterLaunchUs;
+        t = rounds * (stages * f.full + f.end) + last + (E ? kInt8FindUs : 0.0);
+        if (E && form != kInt8Deep128) rate *= kInt8ExpertBytes;
     } else {
         const double share = tiles / 256.0;
-        t = (E ? kInt8ExpertStage : 1.0) * std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
+        t = std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
     }
-    t = std::max(t, (used * (double)N * (double)K + (double)T * (double)K) / (f.bytes_us * (E && f.persistent ? kInt8ExpertBytes : 1.0)));
-    if (E && f.persistent) t += kInt8FindUs;
-    if (f.places == 16) t += tiles * (double)std::min<int64_t>(T, 16) * (double)K / kInt8TokensUs;
+    t = std::max(t, (used * (double)N * (double)K + (double)T * (double)K) / rate);
+    if (form == kInt8Few) t += tiles * (double)std::min<int64_t>(T, 16) * (double)K / kInt8TokensUs;
     if (splits > 1) t += f.join + (double)int8_part_bytes(f, T, N, splits) * 2.0 / f.join_bytes_us;
     return f.launch + t;
 }
@@ -83,7 +90,7 @@ inline int64_t int8_grid(int form, int64_t T, int64_t N, int64_t E, int splits) 
     const int64_t blocks = E == 0 ? cdiv(T, f.places) : T / f.places + std::min(E, T);
     return blocks * cdiv(N, f.channels) * splits;
 }
-// (a launch has less than 2^32 threads; the persistent forms loop)
+// (a launch has less than 2^32 threads)
 constexpr int64_t kInt8MostWorkgroups = 0xFFFFFF;   // of 256 threads
 
 struct Int8Plan {
@@ -95,12 +102,12 @@ inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64
     double least = 1e300;
     for (int form = 0; form < kInt8Forms; ++form) {
         const Int8Cost &f = kInt8Costs[form];
-        if (!f.persistent && int8_grid(form, T, N, E, 1) > kInt8MostWorkgroups) continue;
-        const bool cut = E == 0 && form >= kInt8Mid32 && form <= kInt8Mid96;
+        if (!f.looped && int8_grid(form, T, N, E, 1) > kInt8MostWorkgroups) continue;
+        const bool cut = E == 0 && form >= kInt8Mid32 && form <= kInt8Deep128;
         for (int s = 1; s <= (cut ? kInt8MaxSplits : 1); ++s) {
             // a range has two stages at least, and only grids of less than four rounds are cut
             if (s > 1 && (cdiv(K, 128) < 2 * s || cdiv(N, f.channels) * cdiv(T, f.places) > 1024 || int8_part_bytes(f, T, N, s) > part_bytes)) break;
-            const double t = int8_cost(f, T, N, K, E, s);
+            const double t = int8_cost(form, T, N, K, E, s);
             if (t < least) {
                 least = t;
                 best = Int8Plan{form, s};

@@ -18,13 +18,13 @@ __device__ __forceinline__ int here(int v) {
     return v;
 }
 
-// WR x WC waves, each with RB blocks of 16 channels times TB blocks of 16 places; stages of 128 k, two of them in LDS; then the scale,
+// WR x WC waves, each with RB blocks of 16 channels times TB blocks of 16 places; stages of 128 k, NBUF of them in LDS; then the scale,
 // zero-point, token scale and token sum of the tile's rows for two tiles, and for each wave 16 rows of outputs.
-template <int RB, int TB, int WR, int WC>
+template <int RB, int TB, int WR, int WC, int NBUF>
 struct Int8Tile {
     static constexpr int NW = WR * WC, TN = 16 * RB * WR, TM = 16 * TB * WC;
     static constexpr int STAGE = (TN + TM) * 128;
-    static constexpr int PARAMS = 2 * STAGE, PARAM_SET = (TN + TM) * 8;
+    static constexpr int PARAMS = NBUF * STAGE, PARAM_SET = (TN + TM) * 8;
     static constexpr int OUT = PARAMS + 2 * PARAM_SET, OS = RB * 32 + 16;   // OS: bytes of a row of outputs
     static constexpr int LDS = OUT + NW * 16 * OS;
 };
@@ -36,11 +36,12 @@ __device__ __forceinline__ bool in_quarters(int total) { return total >= 256 && 
 
 // Persistent: workgroup i takes tiles i, i + gridDim.x, ...; the first stages of a tile are requested before the outputs of the one
 // before are formed.
-template <bool R8, int RB, int TB, int WR, int WC, int WGS>
-__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Part part) {
+// CUT: K is cut into ranges whose sums go to ranges.part, as mq_int8_mid.hip leaves them.
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS, bool CUT>
+__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Part part, Int8Ranges ranges) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    typedef Int8Tile<RB, TB, WR, WC> T;
+    typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
     typedef __attribute__((address_space(1))) void *global_ptr;
     constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL, NM = RB * TB;
     static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0 && T::TN % 64 == 0 && T::TM % 64 == 0 && T::LDS + 4 * (kMaxExperts + 1) <= 160 * 1024, "");
@@ -66,21 +67,23 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     struct Tile {
         Block b;
         int n0;
+        int range;
     };
+    const int splits = CUT ? ranges.splits : 1, stages = (a.K + 127) / 128;
     auto unit_at = [&](int lid) {
         constexpr int GROUP = 4;
         const int width = GROUP * tiles_n;
         const int first_m = lid / width * GROUP;
         const int gsz = min(tiles_m - first_m, GROUP);
         const int block = first_m + lid % width % gsz, n0 = lid % width / gsz * unit;
-        if (!a.offsets) return Tile{Block{0, block * unit, min(unit, a.T - block * unit)}, n0};
-        return Tile{find_block(a.T, a.E, block, unit, [&](int e) { return bounds[e]; }), n0};
+        if (!a.offsets) return Tile{Block{0, block * unit, min(unit, a.T - block * unit)}, n0, 0};
+        return Tile{find_block(a.T, a.E, block, unit, [&](int e) { return bounds[e]; }), n0, 0};
     };
     // the first tile from id on, in steps of the grid, that is not empty (quarters may be): id is left at it, or past the last
     auto tile_from = [&](int &id) {
         Tile t = {};
-        for (; id < total; id += (int)gridDim.x) {
-            const int lid = (int)xcd_contiguous_id(id, total);
+        for (; id < total * splits; id += (int)gridDim.x) {
+            const int at = (int)xcd_contiguous_id(id, total * splits), lid = CUT ? at % total : at;
             t = unit_at(part == kInt8Quarters ? units - rest + lid / 4 : lid);
             if (part == kInt8Quarters) {
                 const int down = (lid & 1) * T::TM;
@@ -88,6 +91,7 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
                 t.b.count = min(t.b.count - down, T::TM);
                 t.n0 += (lid >> 1 & 1) * T::TN;
             }
+            if (CUT) t.range = at / total;
             if (t.b.count > 0 && t.n0 < a.N) break;
         }
         return t;
@@ -101,6 +105,7 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     for (int i = 1; i < CL; ++i) coff[i] = coff[0] + (uint32_t)(8 * NW * i) * (uint32_t)a.K;
     __amdgpu_buffer_rsrc_t rC, rX;
     uint32_t xoff[XL];
+    int k_begin = 0, k_end = a.K;   // of the tile that is being requested
 
     // Load i of the stage at k0 into buffer `buf`.  INSIDE: the stage lies within the rows; otherwise what stands past their end is
     // requested out of range, which the buffer unit answers with zeros, so that every stage has as many loads in flight.
@@ -111,10 +116,11 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         if constexpr (INSIDE)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, off, k0, 0, 0);
         else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, k0 + col < a.K ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)to, 16, k0 + col < k_end ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
     };
     // The tokens whose rows and parameters this lane requests of a tile: found while the tile before is multiplied.
-    static_assert((T::TN + T::TM) / 64 == NW, "a wave fetches the parameters of 64 rows");
+    static_assert((T::TN + T::TM) / 64 <= NW, "a wave fetches the parameters of 64 rows");
+    const bool fetches = wave < (T::TN + T::TM) / 64;
     int tokens[XL], param_row;   // (as they stand in rows; nothing waits for them before begin)
     auto look = [&](const Tile &t) {
         const int lane = here(threadIdx.x & 63);
@@ -125,11 +131,15 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         if (a.rows) {
 #pragma unroll
             for (int i = 0; i < XL; ++i) tokens[i] = a.rows[tokens[i]];
-            if (wave >= T::TN / 64) param_row = a.rows[param_row];
+            if (fetches && wave >= T::TN / 64) param_row = a.rows[param_row];
         }
     };
     // A tile's parameters (set `set`) and its first two stages.
     auto begin = [&](const Tile &t, int set) {
+        if (CUT) {
+            k_begin = (int)((int64_t)stages * t.range / splits) * 128;
+            k_end = min(a.K, (int)((int64_t)stages * (t.range + 1) / splits) * 128);
+        }
         rC = make_rsrc(a.codes + ((int64_t)t.b.expert * a.N + t.n0) * a.K, (uint64_t)(a.N - t.n0) * a.K);
         const int base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
         rX = make_rsrc(a.Xq + (int64_t)base * a.K, (uint64_t)(a.M - base) * a.K);
@@ -144,12 +154,14 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
             const int m = min(max(param_row, 0), a.M - 1);
             one = a.scale + m, two = a.sum + m;
         }
-        __builtin_amdgcn_global_load_lds((global_ptr)one, (lds_ptr)to, 4, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)two, (lds_ptr)(to + 256), 4, 0, 0);
+        if (fetches) {
+            __builtin_amdgcn_global_load_lds((global_ptr)one, (lds_ptr)to, 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)two, (lds_ptr)(to + 256), 4, 0, 0);
+        }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < NBUF; ++s)
 #pragma unroll
-            for (int i = 0; i < LPS; ++i) issue_one(std::false_type{}, s * 128, s, i);
+            for (int i = 0; i < LPS; ++i) issue_one(std::false_type{}, k_begin + s * 128, s, i);
     };
 
     // operands of half t of a stage; + 2048 per block of 16 rows
@@ -168,11 +180,11 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
     // last of these reads, not right behind it.)
     auto half = [&](auto inside_tag, auto t_tag, int k0, int buf) {
         constexpr int t = decltype(t_tag)::value;
-        const uint8_t *src = smem + (t == 0 ? buf : 1 - buf) * T::STAGE;
+        const uint8_t *src = smem + (t == 0 ? buf : buf + 1 == NBUF ? 0 : buf + 1) * T::STAGE;
         static_for<NM>([&](auto q_tag) {
             constexpr int q = decltype(q_tag)::value, tb = q / RB, rb = q % RB;
             mfma_i8_acc(acc[rb][tb], wf[t][rb], xf[tb]);
-            if constexpr (t == 1 && q == RB - 1) stage_barrier<0, 0>();   // the next stage has landed, every wave has read this one
+            if constexpr (t == 1 && q == RB - 1) stage_barrier<(NBUF - 2) * LPS, 0>();   // the next stage has landed, every wave has read this one
             if constexpr (rb == RB - 1) xf[tb] = *reinterpret_cast<const i32x4 *>(src + xa[1 - t] + tb * 2048);
             static_for<RB>([&](auto j_tag) {
                 constexpr int j = decltype(j_tag)::value;
@@ -184,7 +196,7 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
             });
             static_for<t == 1 ? LPS : 0>([&](auto l_tag) {
                 constexpr int l = decltype(l_tag)::value;
-                if constexpr (q == RB + 1 + l * (NM / 2) / LPS) issue_one(inside_tag, k0 + 256, buf, l);
+                if constexpr (q == RB + 1 + l * (NM / 2) / LPS) issue_one(inside_tag, k0 + 128 * NBUF, buf, l);
             });
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -268,9 +280,18 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         }
     };
 
+    auto leave = [&](const Tile &t) {   // (of a dense product)
+        const int tile = t.n0 / T::TN * tiles_m + t.b.place / T::TM;
+        i32x4 *to = ranges.part + ((int64_t)(t.range * total + tile) * NW + wave) * (RB * TB * 64) + lane;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) to[(rb * TB + tb) * 64] = acc[rb][tb];
+    };
+
     int id = blockIdx.x, set = 0;
     Tile cur = tile_from(id);
-    if (id >= total) return;
+    if (id >= total * splits) return;
     look(cur);
     begin(cur, set);
     for (;;) {
@@ -279,30 +300,32 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
-        stage_barrier<LPS, 0>();
+        stage_barrier<(NBUF - 1) * LPS, 0>();
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) wf[0][rb] = signed_codes<R8>(*reinterpret_cast<const i32x4 *>(smem + ca[0] + rb * 2048));
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) xf[tb] = *reinterpret_cast<const i32x4 *>(smem + xa[0] + tb * 2048);
         const Tile next = tile_from(next_id);
-        if (next_id < total) look(next);
-        int k0 = 0, buf = 0;
+        if (next_id < total * splits) look(next);
+        int k0 = k_begin, buf = 0;
         auto stage = [&](auto inside_tag) {
             half(inside_tag, std::integral_constant<int, 0>{}, k0, buf);
             half(inside_tag, std::integral_constant<int, 1>{}, k0, buf);
             k0 += 128;
-            buf = 1 - buf;
+            buf = buf + 1 == NBUF ? 0 : buf + 1;
         };
-        while (k0 + 384 <= a.K) stage(std::true_type{});
-        while (k0 < a.K) stage(std::false_type{});
+        while (k0 + 128 * (NBUF + 1) <= k_end) stage(std::true_type{});
+        while (k0 < k_end) stage(std::false_type{});
         mfma16_settle();
         stage_barrier<0, 0>();   // the buffers are free
-        if (next_id < total) begin(next, 1 - set);
-        if (a.gate)
+        if (next_id < total * splits) begin(next, 1 - set);
+        if (CUT)
+            leave(cur);
+        else if (a.gate)
             finish(std::true_type{}, cur, set);
         else
             finish(std::false_type{}, cur, set);
-        if (next_id >= total) break;
+        if (next_id >= total * splits) break;
         id = next_id;
         cur = next;
         set = 1 - set;
@@ -314,35 +337,48 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
 
 namespace {
 
-template <bool R8, int RB, int TB, int WR, int WC, int WGS>
-mq_status launch_tile(const Int8Args &a, Int8Part part, hipStream_t st) {
-    typedef Int8Tile<RB, TB, WR, WC> T;
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS, bool CUT = false>
+mq_status launch_tile(const Int8Args &a, Int8Form form, Int8Part part, hipStream_t st, const Int8Ranges &ranges = {nullptr, 1}) {
+    typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
     static_assert(T::TN == T::TM && (T::TM == 128 || T::TM == 256), "the forms of mq_int8_plan.h");
     const int64_t unit = part == kInt8Quarters ? 256 : T::TM, tiles_n = cdiv(a.N, unit);
-    const int64_t tiles = int8_grid(unit == 128 ? kInt8Tile128 : kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
-    if (tiles > 0x7FFFFF00) return MQ_ERR_SHAPE;
-    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, WGS>;
+    const int64_t tiles = int8_grid(part == kInt8Quarters ? kInt8Tile256 : form, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
+    if (tiles * ranges.splits > 0x7FFFFF00) return MQ_ERR_SHAPE;
+    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, NBUF, WGS, CUT>;
     const int lds = T::LDS + (a.offsets ? (a.E + 1) * 4 : 0);
     if (!allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
     const int64_t most = 256 * WGS;   // workgroups that fit the GPU
-    kernel<<<dim3((unsigned)std::min(part == kInt8Quarters ? most : tiles, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n, part);
+    kernel<<<dim3((unsigned)std::min(part == kInt8Quarters ? most : tiles * ranges.splits, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n, part, ranges);
     return launch_status();
 }
 
 template <bool R8>
-mq_status launch_tiles(const Int8Args &a, int places, hipStream_t st) {
-    if (places == 128) return launch_tile<R8, 4, 4, 2, 2, 2>(a, kInt8All, st);
+mq_status launch_deep(const Int8Args &a, Int8Part part, hipStream_t st) {
+    return launch_tile<R8, 2, 4, 4, 2, 4, 1>(a, kInt8Deep128, part, st);
+}
+
+template <bool R8>
+mq_status launch_tiles(const Int8Args &a, Int8Form form, int splits, void *part, hipStream_t st) {
+    if (form == kInt8Deep128) {
+        if (splits == 1) return launch_deep<R8>(a, kInt8All, st);
+        const Int8Ranges ranges{static_cast<i32x4 *>(part), splits};
+        const mq_status s = launch_tile<R8, 2, 4, 4, 2, 4, 1, true>(a, form, kInt8All, st, ranges);
+        return s != MQ_OK ? s : launch_int8_join<2, 4, 4, 2>(a, ranges, st);
+    }
+    if (form == kInt8Tile128) return launch_tile<R8, 4, 4, 2, 2, 2, 2>(a, form, kInt8All, st);
+    const int64_t tiles = int8_grid(form, a.T, a.N, a.offsets ? a.E : 0, 1), rest = tiles % 256;
+    if (tiles < 256 || (!a.offsets && (rest == 0 || rest > kInt8QuarterTiles))) return launch_tile<R8, 4, 8, 4, 2, 2, 1>(a, form, kInt8All, st);
     // (with experts the number of tiles is a bound: the launch for the rest may find nothing to do)
-    const int64_t tiles = int8_grid(kInt8Tile256, a.T, a.N, a.offsets ? a.E : 0, 1);
-    if (tiles < 256 || (!a.offsets && (tiles % 256 == 0 || tiles % 256 > kInt8QuarterTiles))) return launch_tile<R8, 4, 8, 4, 2, 1>(a, kInt8All, st);
-    const mq_status s = launch_tile<R8, 4, 8, 4, 2, 1>(a, kInt8Rounds, st);
-    return s != MQ_OK ? s : launch_tile<R8, 4, 4, 2, 2, 2>(a, kInt8Quarters, st);
+    const mq_status s = launch_tile<R8, 4, 8, 4, 2, 2, 1>(a, form, kInt8Rounds, st);
+    if (s != MQ_OK) return s;
+    if (!a.offsets && rest <= kInt8DeepQuarterTiles) return launch_deep<R8>(a, kInt8Quarters, st);
+    return launch_tile<R8, 4, 4, 2, 2, 2, 2>(a, kInt8Tile128, kInt8Quarters, st);
 }
 
 }  // namespace
 
-mq_status launch_int8_tiles(const Int8Args &a, int places, hipStream_t st) {
-    return a.offset != 0.f ? launch_tiles<true>(a, places, st) : launch_tiles<false>(a, places, st);
+mq_status launch_int8_tiles(const Int8Args &a, Int8Form form, int splits, void *part, hipStream_t st) {
+    return a.offset != 0.f ? launch_tiles<true>(a, form, splits, part, st) : launch_tiles<false>(a, form, splits, part, st);
 }
 
 }  // namespace mq

@@ -15,7 +15,7 @@ using namespace mq;
 extern "C" void int8_form(int64_t T, int64_t N, int64_t K, int64_t E, int64_t part_bytes, int64_t *out) {
     const Int8Plan p = make_int8_plan(T, N, K, E, part_bytes);
     const Int8Cost &f = kInt8Costs[p.form];
-    out[0] = p.form, out[1] = p.splits, out[2] = int8_grid(p.form, T, N, E, p.splits), out[3] = f.persistent;
+    out[0] = p.form, out[1] = p.splits, out[2] = int8_grid(p.form, T, N, E, p.splits), out[3] = f.looped;
     out[4] = E == 0 ? int8_part_bytes(f, T, N, p.splits) : 0;
     out[5] = f.places == 256 && out[2] >= 256 && out[2] % 256 != 0 && out[2] % 256 <= kInt8QuarterTiles;
     out[6] = int8_single(T, N, K, E) ? 1 + int8_single_wide(T, N, E) : 0;
@@ -24,10 +24,10 @@ extern "C" int64_t int8_part_limit(void) { return kInt8PartBytes; }
 extern "C" int64_t int8_most_workgroups(void) { return kInt8MostWorkgroups; }
 '''
 
-FORMS = ["few", "mid32", "mid64", "mid96", "tile128", "tile256"]
-# grid: workgroups, or tiles where they are looped over (`persistent`); part: bytes of partial sums; quarters: the last round of 256-tiles is
+FORMS = ["few", "mid32", "mid64", "mid96", "deep128", "tile128", "tile256"]
+# grid: workgroups, or tiles where they are looped over (`looped`); part: bytes of partial sums; quarters: the last round of 256-tiles is
 # done in 128-tiles (dense products); single: 0, or 1 / 2 where bf16 tokens are quantized by workgroups of 16 / 32 channels
-Form = namedtuple("Form", "name ranges grid persistent part quarters single")
+Form = namedtuple("Form", "name ranges grid looped part quarters single")
 
 
 @functools.lru_cache(maxsize=None)

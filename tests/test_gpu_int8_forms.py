@@ -12,15 +12,17 @@ DENSE = [
     ("few", False, False, 16, 333, 1040, 8, None), ("few", False, False, 9, 1028, 2064, 4, "silu"), ("few", False, False, 5, 4099, 4112, 8, None),
     ("mid32", False, False, 50, 4099, 528, 8, None), ("mid32", False, False, 70, 2304, 1040, 4, "gelu"), ("mid32", False, False, 33, 5001, 16, 8, None),
     ("mid32", True, False, 33, 2051, 4112, 8, None), ("mid32", True, False, 30, 4352, 4112, 2, "silu"), ("mid32", True, False, 13, 70, 8208, 8, None),
-    ("mid64", False, False, 511, 4099, 272, 8, None), ("mid64", False, False, 180, 9472, 400, 6, "gelu"),
-    ("mid64", True, False, 127, 2050, 4112, 8, "gelu"), ("mid64", True, False, 250, 1027, 4112, 3, None),
-    ("mid96", False, False, 180, 9001, 1040, 8, None), ("mid96", False, False, 770, 9472, 16, 5, "silu"),
-    ("mid96", True, False, 77, 4099, 8208, 8, None), ("mid96", True, False, 90, 4352, 8208, 4, "silu"),
-    ("tile128", False, False, 511, 4099, 16, 8, None), ("tile128", False, False, 1030, 2304, 400, 4, "gelu"), ("tile128", False, False, 250, 9473, 400, 8, None),
+    ("mid64", False, False, 511, 4099, 272, 8, None), ("mid64", False, False, 180, 9472, 528, 6, "gelu"),
+    ("mid64", True, False, 100, 2050, 4112, 8, "gelu"), ("mid64", True, False, 300, 1027, 4112, 3, None),
+    ("mid96", False, False, 180, 9001, 2064, 8, None), ("mid96", False, False, 770, 9472, 16, 5, "silu"),
+    ("mid96", True, False, 180, 4352, 8208, 4, "silu"), ("mid96", True, False, 77, 4099, 8208, 8, None),
+    ("deep128", False, False, 511, 4099, 1040, 8, None), ("deep128", False, False, 200, 9472, 1040, 4, "gelu"), ("deep128", False, False, 401, 5001, 1040, 8, None),
+    ("deep128", True, False, 770, 1027, 8208, 8, None), ("deep128", True, False, 200, 4352, 8208, 6, "silu"), ("deep128", True, False, 255, 4099, 8208, 2, None),
+    ("tile128", False, False, 511, 4099, 16, 8, None), ("tile128", False, False, 1030, 5002, 144, 4, "gelu"), ("tile128", False, False, 180, 14335, 272, 8, None),
     ("tile128", False, False, 4100, 5001, 144, 8, None), ("tile128", False, False, 1030, 14336, 272, 8, "silu"),
     ("tile256", False, False, 1030, 9001, 272, 8, None), ("tile256", False, False, 2050, 4352, 272, 7, "gelu"), ("tile256", False, False, 600, 14336, 16, 8, None),
     ("tile256", False, False, 3000, 9001, 144, 8, None), ("tile256", False, False, 3000, 14336, 48, 4, "silu"),
-    ("tile256", False, True, 4100, 9001, 144, 8, None), ("tile256", False, True, 4100, 9472, 144, 2, "gelu"),
+    ("tile256", False, True, 4100, 9001, 144, 8, None), ("tile256", False, True, 4100, 9472, 144, 2, "gelu"), ("tile256", False, True, 3900, 4400, 528, 8, None),
 ]
 # tokens, channels, values, whether a workgroup has 32 channels: quantized by the product's own workgroups
 SINGLE = [(1, 7, 16, False), (1, 4096, 4096, False), (2, 333, 8208, False), (3, 1027, 16384, False), (1, 14336, 1040, True), (2, 12290, 272, True), (3, 16385, 400, True)]
@@ -28,8 +30,10 @@ SINGLE = [(1, 7, 16, False), (1, 4096, 4096, False), (2, 333, 8208, False), (3, 
 EXPERTS = [
     ("few", 8, [5, 0, 0, 1, 0, 2], 7, 1027, 1040, 8, None), ("few", 40, [0] * 37 + [3, 1, 1], 4, 2304, 528, 4, "gelu"), ("few", 3, [40, 1, 49], 60, 1027, 4112, 8, None),
     ("mid32", 8, [3, 0, 9, 1, 0, 0, 17], 20, 9001, 528, 8, None), ("mid32", 40, [1, 2, 3] * 10 + [20, 0, 7], 50, 4098, 528, 8, "silu"), ("mid32", 8, [33, 1, 0, 64, 2, 90], 100, 9001, 4112, 2, None),
-    ("mid64", 3, [100, 0, 301], 300, 2304, 2064, 8, "gelu"), ("mid64", 8, [700, 0, 0, 0, 70], 300, 1027, 4112, 8, None),
-    ("tile128", 3, [128, 640, 2], 500, 2304, 528, 8, "silu"), ("tile128", 8, [1, 127, 129, 0, 0, 256, 257], 333, 2305, 528, 8, None), ("tile128", 40, [150] * 40, 2000, 9001, 144, 4, None),
+    ("mid64", 3, [100, 0, 301], 300, 2304, 2064, 8, "gelu"), ("mid64", 8, [1400, 0, 0, 0, 100, 0, 0, 0], 300, 1027, 16, 8, None),
+    ("mid96", 8, [100, 1, 0, 150, 97, 0, 53], 300, 4099, 528, 8, None),
+    ("deep128", 3, [128, 640, 2], 500, 2304, 4112, 8, "silu"), ("deep128", 8, [1, 127, 129, 0, 0, 256, 257, 0], 333, 2304, 528, 8, None),
+    ("tile128", 3, [1000, 1, 499], 500, 4352, 144, 8, "silu"), ("tile128", 40, [150] * 40, 2000, 9001, 144, 4, None),
     ("tile256", 8, [300, 0, 1, 600, 255, 256, 88, 0], 1000, 4099, 528, 8, None), ("tile256", 3, [2000, 4000, 0], 5000, 2304, 144, 8, "gelu"),
     ("tile256", 3, [1, 5998, 1], 3000, 9002, 144, 8, "silu"), ("tile256", 8, [3000, 0, 2, 0, 0, 1480, 1, 1517], 3000, 9001, 144, 4, None),
 ]
@@ -46,14 +50,14 @@ def test_sizes_take_the_form_that_they_stand_for(case):
 
 
 def test_all_forms_are_there():
-    assert {c[:3] for c in DENSE} >= {(f, False, False) for f in int8_plans.FORMS} | {("mid32", True, False), ("mid64", True, False), ("mid96", True, False), ("tile256", False, True)}
+    assert {c[:3] for c in DENSE} >= {(f, False, False) for f in int8_plans.FORMS} | {("mid32", True, False), ("mid64", True, False), ("mid96", True, False), ("deep128", True, False), ("tile256", False, True)}
     for T, N, K, wide in SINGLE:
         assert int8_plans.form(T, N, K).single == (2 if wide else 1)
     for name, E, counts, M, N, K, r, gate in EXPERTS:
         f = int8_plans.form(sum(counts), N, K, E)
         assert f.name == name and not f.single, (name, E, N, K, f)
         assert len(counts) <= E
-    assert {c[0] for c in EXPERTS} == set(int8_plans.FORMS) - {"mid96"}
+    assert {c[0] for c in EXPERTS} == set(int8_plans.FORMS)
 
 
 # ---- on the GPU ----------------------------------------------------------------------------------------------------------

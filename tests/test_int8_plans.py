@@ -19,14 +19,14 @@ def test_launches_fit(K, E):
     """Less than 2^32 threads, 256 to a workgroup, where tiles are not looped over."""
     for T, N in SIZES:
         f = int8_plans.form(T, N, K, E)
-        assert f.persistent or f.grid <= int8_plans.most_workgroups() < 1 << 24, (T, N, f)
+        assert f.looped or f.grid <= int8_plans.most_workgroups() < 1 << 24, (T, N, f)
 
 
 def test_partial_sums_fit():
     for T, N, K, E in drawn():
         f = int8_plans.form(T, N, K, E)
         assert f.part <= int8_plans.part_limit()
-        assert f.ranges == 1 or (E == 0 and f.name.startswith("mid") and -(-K // 128) >= 2 * f.ranges)
+        assert f.ranges == 1 or (E == 0 and f.name in ("mid32", "mid64", "mid96", "deep128") and -(-K // 128) >= 2 * f.ranges)
         # the form of a workspace that was sized for the call, and of one that has no room
         assert int8_plans.form(T, N, K, E, f.part)[:2] == f[:2]
         assert int8_plans.form(T, N, K, E, 0).ranges == 1

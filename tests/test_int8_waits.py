@@ -35,4 +35,4 @@ def test_products_of_the_tiles(tmp_path):
             products += sum(c[4] for c in code)
             loads += sum(c[0].endswith(" lds") for c in code)
             assert not violations(code), (m.group(1), violations(code)[:3])
-    assert kernels == 4 and products > 300 and loads > 100
+    assert kernels == 8 and products > 300 and loads > 100
