@@ -70,14 +70,24 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         int range;
     };
     const int splits = CUT ? ranges.splits : 1, stages = (a.K + 127) / 128;
+    // Four blocks of places at a time, all channels for them; products by expert: of one expert, whose codes are then read from memory once.
     auto unit_at = [&](int lid) {
         constexpr int GROUP = 4;
-        const int width = GROUP * tiles_n;
-        const int first_m = lid / width * GROUP;
-        const int gsz = min(tiles_m - first_m, GROUP);
-        const int block = first_m + lid % width % gsz, n0 = lid % width / gsz * unit;
-        if (!a.offsets) return Tile{Block{0, block * unit, min(unit, a.T - block * unit)}, n0, 0};
-        return Tile{find_block(a.T, a.E, block, unit, [&](int e) { return bounds[e]; }), n0, 0};
+        int first = 0, blocks = tiles_m;   // the expert's
+        Block b{0, 0, a.T};
+        if (a.offsets) {
+            b = find_block(a.T, a.E, lid / tiles_n, unit, [&](int e) { return bounds[e]; });
+            const int lo = min(max(bounds[b.expert], 0), a.T), hi = min(max(bounds[b.expert + 1], lo), a.T);
+            if (b.count <= 0) return Tile{b, 0, 0};
+            first = lid / tiles_n - (b.place - lo) / unit;
+            blocks = (int)(((uint32_t)(hi - lo) + (uint32_t)unit - 1u) / (uint32_t)unit);
+            b.place = lo;
+            b.count = hi - lo;
+        }
+        const int local = lid - first * tiles_n, width = GROUP * tiles_n;
+        const int first_m = local / width * GROUP, gsz = min(blocks - first_m, GROUP);
+        const int down = (first_m + local % width % gsz) * unit;
+        return Tile{Block{b.expert, b.place + down, min(unit, b.count - down)}, local % width / gsz * unit, 0};
     };
     // the first tile from id on, in steps of the grid, that is not empty (quarters may be): id is left at it, or past the last
     auto tile_from = [&](int &id) {
