@@ -11,11 +11,12 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int64_t kInt8MaxK = 131072;     // 127 * 128 * K stays below 2^31
 constexpr int64_t kMaxExperts = 1024;
+constexpr int64_t kInt8Line = 128;        // of the L2: a stage of 128 k of a row that begins elsewhere takes two of them
 
 // One product: Y[p, n] of T places, place p holding token rows[p] (or p) and belonging to the expert e with
 // offsets[e] <= p < offsets[e + 1] (or to the only one).
 struct Int8Args {
-    const int8_t *Xq;        // [M, K]
+    const int8_t *Xq;        // [M, K], rows ldq bytes apart
     const float *scale;      // [M]
     const int32_t *sum;      // [M]
     const int32_t *rows;     // [T] or null
@@ -24,6 +25,7 @@ struct Int8Args {
     const float *alpha, *zero;  // [E, N]
     uint16_t *Y;             // [T, N], with a gate [T, N / 2]
     int M, T, N, K, E;
+    int ldq;                 // K or more; the library's own rows begin at lines of 128 bytes (kInt8Line)
     int gate;                // 0 none, 1 GELU-tanh, 2 SiLU
     float mult, offset;      // 2^(8-r); what the matrix core's signed reading of a code leaves out (128 at r = 8, otherwise 0)
 };
@@ -225,7 +227,7 @@ mq_status launch_int8_join(const Int8Args &a, const Int8Ranges &s, hipStream_t s
     return launch_status();
 }
 
-mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
+mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, int64_t ldq,
                                  float *scale, int32_t *sum, hipStream_t st);
 mq_status launch_int8_few(const Int8Args &a, hipStream_t st);
 // the same on bf16 tokens X [M, K], for up to kInt8SinglePlaces places and kInt8SingleK values a token

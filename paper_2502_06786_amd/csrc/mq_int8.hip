@@ -13,7 +13,7 @@ namespace mq {
 // rows: null, or the row of X that row m of the result is made of (rows are data: whatever they hold, they stay below X_rows).
 template <int TPR, int V, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *__restrict__ X, int64_t M, int K, int64_t ldx,
-                                                                const int32_t *__restrict__ rows, int X_rows, int8_t *__restrict__ Xq,
+                                                                const int32_t *__restrict__ rows, int X_rows, int8_t *__restrict__ Xq, int64_t ldq,
                                                                 float *__restrict__ scale, int32_t *__restrict__ sum) {
     constexpr int WAVES = TPR / 64;  // to a row
     __shared__ uint32_t tops[BLOCK / 64];
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
     for (int i = 0; i < V; ++i) {
         const int c = t + i * TPR;
         const u32x2 codes = token_codes(v[i], ts, total);
-        if (live && c * 8 < K) *reinterpret_cast<u32x2 *>(Xq + m * K + c * 8) = codes;
+        if (live && c * 8 < K) *reinterpret_cast<u32x2 *>(Xq + m * ldq + c * 8) = codes;
     }
     total = sum_of_wave(total);
     if constexpr (WAVES > 1) {
@@ -66,14 +66,14 @@ __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *
 namespace {
 
 template <int TPR, int V, int BLOCK>
-mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, float *scale,
+mq_status launch_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, int64_t ldq, float *scale,
                         int32_t *sum, hipStream_t st) {
     // (a launch has less than 2^32 threads)
     constexpr int64_t most = 0xFFFFFFFFll / BLOCK * (BLOCK / TPR);
     for (int64_t m = 0; m < M; m += most) {
         const int64_t n = std::min(M - m, most);
         quantize_tokens_kernel<TPR, V, BLOCK><<<dim3((unsigned)cdiv(n, BLOCK / TPR)), dim3(BLOCK), 0, st>>>(
-            rows ? X : X + m * ldx, n, (int)K, ldx, rows ? rows + m : nullptr, (int)X_rows, Xq + m * K, scale + m, sum + m);
+            rows ? X : X + m * ldx, n, (int)K, ldx, rows ? rows + m : nullptr, (int)X_rows, Xq + m * ldq, ldq, scale + m, sum + m);
     }
     return launch_status();
 }
@@ -85,7 +85,7 @@ struct Int8Layout {
 Int8Layout int8_layout(int64_t M, int64_t K) {
     Int8Layout l;
     size_t off = 0;
-    l.codes = off, off += align256((size_t)M * K);
+    l.codes = off, off += align256((size_t)M * (cdiv(K, kInt8Line) * kInt8Line));
     l.scale = off, off += align256((size_t)M * 4);
     l.sum = off, off += align256((size_t)M * 4);
     l.part = off;
@@ -132,7 +132,7 @@ Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, 
     a.M = (int)M;
     a.T = (int)T;
     a.N = (int)N;
-    a.K = (int)K;
+    a.K = a.ldq = (int)K;
     a.E = (int)E;
     a.gate = !(flags & MQ_FLAG_GATED) ? 0 : (flags & MQ_FLAG_FFN_SILU) ? 2 : 1;
     a.mult = (float)(1 << (8 - r));
@@ -147,11 +147,12 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
     if (int8_single(a.T, a.N, a.K, a.offsets ? a.E : 0)) return launch_int8_single(a, X, st);
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
     int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
+    a.ldq = (int)(cdiv(a.K, kInt8Line) * kInt8Line);
     float *scale = reinterpret_cast<float *>(base + l.scale);
     int32_t *sum = reinterpret_cast<int32_t *>(base + l.sum);
     // gathered tokens past 2 GiB are quantized in the order of the places: the kernels address those that they gather with 32 bits
-    const bool placed = a.rows && (int64_t)a.M * a.K > 0x7FFFFFFF;
-    const mq_status s = launch_quantize_tokens(X, placed ? a.T : a.M, a.K, a.K, placed ? a.rows : nullptr, a.M, Xq, scale, sum, st);
+    const bool placed = a.rows && (int64_t)a.M * a.ldq > 0x7FFFFFFF;
+    const mq_status s = launch_quantize_tokens(X, placed ? a.T : a.M, a.K, a.K, placed ? a.rows : nullptr, a.M, Xq, a.ldq, scale, sum, st);
     if (s != MQ_OK) return s;
     if (placed) {
         a.rows = nullptr;
@@ -165,14 +166,14 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
 
 }  // namespace
 
-mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq,
+mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, int64_t ldq,
                                  float *scale, int32_t *sum, hipStream_t st) {
     // With few rows a workgroup to each, which is done sooner: 16 tokens of 4096 values 4.6 -> 3.9 us; with many the fewest lanes that hold a row.
-    if (M <= 512 && K <= 4096) return launch_tokens<256, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
-    if (M <= 256 && K <= 16384) return launch_tokens<1024, 2, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
-    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
-    if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
-    return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, scale, sum, st);
+    if (M <= 512 && K <= 4096) return launch_tokens<256, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (M <= 256 && K <= 16384) return launch_tokens<1024, 2, 1024>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
 }
 
 size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K, bool grouped) {
@@ -195,7 +196,7 @@ extern "C" mq_status mq_quantize_tokens(const uint16_t *X, int64_t M, int64_t K,
     if (M == 0) return MQ_OK;
     if (!X || !Xq || !scale || !sum) return MQ_ERR_NULL;
     if (!aligned16(X) || !aligned16(Xq) || !aligned16(scale) || !aligned16(sum)) return MQ_ERR_ALIGN;
-    return launch_quantize_tokens(X, M, K, ldx, nullptr, M, Xq, scale, sum, static_cast<hipStream_t>(hip_stream));
+    return launch_quantize_tokens(X, M, K, ldx, nullptr, M, Xq, K, scale, sum, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, const int32_t *sum, const uint8_t *codes,

@@ -21,10 +21,10 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(Int8Args a, int tiles
 
     const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
     const int base = a.rows ? 0 : b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
-    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + (int64_t)base * a.K, (uint64_t)(a.M - base) * a.K);
+    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + (int64_t)base * a.ldq, (uint64_t)(a.M - base) * a.ldq);
     const int m = token_of(a, b.place + min(l16, b.count - 1));
     // (a lane takes 32 neighbouring bytes of a row, so that the four of a row take a line; both operands in that order)
-    const uint32_t coff = (uint32_t)l16 * (uint32_t)a.K + 32u * g4, xoff = (uint32_t)(m - base) * (uint32_t)a.K + 32u * g4;
+    const uint32_t coff = (uint32_t)l16 * (uint32_t)a.K + 32u * g4, xoff = (uint32_t)(m - base) * (uint32_t)a.ldq + 32u * g4;
     i32x4 c[DEEP][2], x[DEEP][2];
     auto load = [&](int slot, int k0) {   // past the end of the rows: out of range, zeros
 #pragma unroll

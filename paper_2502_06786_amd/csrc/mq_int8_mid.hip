@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
 
     const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes + ((int64_t)b.expert * a.N + n0) * a.K, (uint64_t)(a.N - n0) * a.K);
     const int64_t base = a.rows ? 0 : b.place;   // (gathered tokens lie within 2 GiB)
-    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + base * a.K, (uint64_t)(a.M - base) * a.K);
+    const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.Xq + base * a.ldq, (uint64_t)(a.M - base) * a.ldq);
     uint32_t coff;
     int col;
     bf16_tile_lane<NW>(wave, lane, 0, (uint32_t)a.K, coff, col);   // (rows of eight 16-byte chunks as there)
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int row = wave * 8 + (lane >> 3) + 8 * NW * i;
-        xoff[i] = (uint32_t)(token_of(a, b.place + min(row, b.count - 1)) - (int)base) * (uint32_t)a.K + (uint32_t)col;
+        xoff[i] = (uint32_t)(token_of(a, b.place + min(row, b.count - 1)) - (int)base) * (uint32_t)a.ldq + (uint32_t)col;
     }
     auto issue = [&](int st, int buf) {   // past the end of the range: out of range, zeros
         const int k0 = st * 128;

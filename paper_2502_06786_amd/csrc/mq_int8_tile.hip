@@ -152,9 +152,9 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         }
         rC = make_rsrc(a.codes + ((int64_t)t.b.expert * a.N + t.n0) * a.K, (uint64_t)(a.N - t.n0) * a.K);
         const int base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
-        rX = make_rsrc(a.Xq + (int64_t)base * a.K, (uint64_t)(a.M - base) * a.K);
+        rX = make_rsrc(a.Xq + (int64_t)base * a.ldq, (uint64_t)(a.M - base) * a.ldq);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)(min(max(tokens[i], 0), a.M - 1) - base) * (uint32_t)a.K + (uint32_t)col;
+        for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)(min(max(tokens[i], 0), a.M - 1) - base) * (uint32_t)a.ldq + (uint32_t)col;
         uint8_t *to = smem + T::PARAMS + set * T::PARAM_SET + wave * 512;
         const void *one, *two;
         if (wave < T::TN / 64) {
