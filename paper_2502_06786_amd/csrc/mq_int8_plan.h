@@ -51,10 +51,10 @@ inline int64_t int8_part_bytes(const Int8Cost &f, int64_t T, int64_t N, int spli
     return splits == 1 ? 0 : cdiv(N, f.channels) * cdiv(T, f.places) * f.channels * f.places * 4 * splits;
 }
 
-// A last round of at most this many 256-tiles is done in quarters of 128 x 128, up to two to a compute unit.
-// (by the form with four stages where there is one to a compute unit at most)
-constexpr int kInt8QuarterTiles = 128, kInt8DeepQuarterTiles = 64;
-constexpr double kInt8QuarterLaunchUs = 3.0;
+// A last round of few 256-tiles is done in quarters of 128 x 128 with four stages: in their first round, or two.
+constexpr int kInt8QuarterTiles = 128;
+constexpr bool int8_quarters(int64_t tiles) { return tiles >= 256 && tiles % 256 != 0 && tiles % 256 <= kInt8QuarterTiles; }
+constexpr double kInt8QuarterUs = 1.0;
 
 // T places of E experts (E = 0: a dense product), in blocks of a form.  How many an expert has is not known here: half a block more than
 // their share is what sizes that vary cost, on average.
@@ -70,8 +70,7 @@ inline double int8_cost(int form, int64_t T, int64_t N, int64_t K, int64_t E, in
         double last = rest > 0 ? stages * (rest > 256.0 ? f.full : f.alone) + f.end : 0.0;
         if (form == kInt8Deep128 && rest > 0) last = stages * std::max(f.alone, f.full * rest / 256.0) + f.end;
         if (form == kInt8Tile256 && rounds > 0 && rest > 0 && rest <= kInt8QuarterTiles)
-            last = rest <= kInt8DeepQuarterTiles ? stages * kInt8Costs[kInt8Deep128].full + kInt8Costs[kInt8Deep128].end + kInt8QuarterLaunchUs
-                                                 : stages * kInt8Costs[kInt8Tile128].full + kInt8Costs[kInt8Tile128].end + kInt8QuarterLaunchUs;
+            last = (rest <= 64.0 ? 1.0 : 2.0) * (stages * kInt8Costs[kInt8Deep128].full + kInt8Costs[kInt8Deep128].end) + kInt8QuarterUs;
         t = rounds * (stages * f.full + f.end) + last + (E ? kInt8FindUs : 0.0);
         if (E && form != kInt8Deep128) rate *= kInt8ExpertBytes;
     } else {

@@ -29,40 +29,26 @@ struct Int8Tile {
     static constexpr int LDS = OUT + NW * 16 * OS;
 };
 
-// What of a product a launch takes: all of its tiles; whole rounds of 256-tiles where the rest is done in quarters; that rest, in 128-tiles
-// (the others then find nothing to do).  How many tiles there are is known on the device only in products by expert, so both launches ask.
-enum Int8Part { kInt8All, kInt8Rounds, kInt8Quarters };
-__device__ __forceinline__ bool in_quarters(int total) { return total >= 256 && total % 256 != 0 && total % 256 <= kInt8QuarterTiles; }
+// Which tiles are taken: `total` of them, `first` counted in units of `unit` places and channels (tiles_m x tiles_n of those in all), each a
+// unit, or (QUARTERS) a quarter of one.
+struct Int8Tiles {
+    int tiles_m, tiles_n, first, total;
+};
 
 // Persistent: workgroup i takes tiles i, i + gridDim.x, ...; the first stages of a tile are requested before the outputs of the one
 // before are formed.
 // CUT: K is cut into ranges whose sums go to ranges.part, as mq_int8_mid.hip leaves them.
-template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS, bool CUT>
-__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Part part, Int8Ranges ranges) {
-#if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
-    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF, bool CUT, bool QUARTERS, typename Bound>
+__device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &tiles, const Int8Ranges &ranges, uint8_t *smem, Bound &&bound) {
     typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
     typedef __attribute__((address_space(1))) void *global_ptr;
     constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL, NM = RB * TB;
     static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0 && T::TN % 64 == 0 && T::TM % 64 == 0 && T::LDS + 4 * (kMaxExperts + 1) <= 160 * 1024, "");
+    constexpr int unit = QUARTERS ? 2 * T::TM : T::TM;
+    const int tiles_m = tiles.tiles_m, tiles_n = tiles.tiles_n, total = tiles.total;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g4 = lane >> 4, l16 = lane & 15, wr = wave / WC, wc = wave % WC;
-
-    // The experts' bounds are kept in LDS, and only blocks that exist are counted: a workgroup's share of a bound on their number would leave
-    // XCDs idle.  Tiles of `unit` places and channels are counted (tiles_m x tiles_n of them).
-    const int unit = part == kInt8Quarters ? 256 : T::TM;
-    const int32_t *bounds = reinterpret_cast<const int32_t *>(smem + T::LDS);
-    if (a.offsets) {
-        for (int e = threadIdx.x; e <= a.E; e += 64 * NW) reinterpret_cast<int32_t *>(smem + T::LDS)[e] = a.offsets[e];
-        __syncthreads();
-        int blocks;
-        find_block(a.T, a.E, 0, unit, [&](int e) { return bounds[e]; }, &blocks);
-        tiles_m = min(max(__builtin_amdgcn_readfirstlane(blocks), 0), tiles_m);
-    }
-    const int units = tiles_m * tiles_n, rest = units % 256;
-    const bool quartered = part != kInt8All && in_quarters(units);
-    const int total = part == kInt8Quarters ? (quartered ? rest * 4 : 0) : quartered ? units - rest : units;
 
     struct Tile {
         Block b;
@@ -76,8 +62,8 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         int first = 0, blocks = tiles_m;   // the expert's
         Block b{0, 0, a.T};
         if (a.offsets) {
-            b = find_block(a.T, a.E, lid / tiles_n, unit, [&](int e) { return bounds[e]; });
-            const int lo = min(max(bounds[b.expert], 0), a.T), hi = min(max(bounds[b.expert + 1], lo), a.T);
+            b = find_block(a.T, a.E, lid / tiles_n, unit, bound);
+            const int lo = min(max(bound(b.expert), 0), a.T), hi = min(max(bound(b.expert + 1), lo), a.T);
             if (b.count <= 0) return Tile{b, 0, 0};
             first = lid / tiles_n - (b.place - lo) / unit;
             blocks = (int)(((uint32_t)(hi - lo) + (uint32_t)unit - 1u) / (uint32_t)unit);
@@ -94,8 +80,8 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         Tile t = {};
         for (; id < total * splits; id += (int)gridDim.x) {
             const int at = (int)xcd_contiguous_id(id, total * splits), lid = CUT ? at % total : at;
-            t = unit_at(part == kInt8Quarters ? units - rest + lid / 4 : lid);
-            if (part == kInt8Quarters) {
+            t = unit_at(tiles.first + (QUARTERS ? lid / 4 : lid));
+            if (QUARTERS) {
                 const int down = (lid & 1) * T::TM;
                 t.b.place += down;
                 t.b.count = min(t.b.count - down, T::TM);
@@ -340,6 +326,35 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
         cur = next;
         set = 1 - set;
     }
+}
+
+// `tiles_m` blocks of places, or with experts a bound on them.  QUARTERS: a last round of few tiles is done in quarters, with four stages in LDS.
+template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS, bool CUT, bool QUARTERS>
+__global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges ranges) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
+    // The experts' bounds are kept in LDS, and only blocks that exist are counted: a workgroup's share of a bound on their number would leave
+    // XCDs idle.
+    int32_t *bounds = reinterpret_cast<int32_t *>(smem + T::LDS);
+    auto bound = [&](int e) { return bounds[e]; };
+    if (a.offsets) {
+        for (int e = threadIdx.x; e <= a.E; e += 64 * T::NW) bounds[e] = a.offsets[e];
+        __syncthreads();
+        int blocks;
+        find_block(a.T, a.E, 0, T::TM, bound, &blocks);
+        tiles_m = min(max(__builtin_amdgcn_readfirstlane(blocks), 0), tiles_m);
+    }
+    const int total = tiles_m * tiles_n, rest = total % 256;
+    const bool quarters = QUARTERS && int8_quarters(total);
+    int8_tiles<R8, RB, TB, WR, WC, NBUF, CUT, false>(a, Int8Tiles{tiles_m, tiles_n, 0, quarters ? total - rest : total}, ranges, smem, bound);
+    if constexpr (QUARTERS) {
+        typedef Int8Tile<2, 4, 4, 2, 4> Q;
+        static_assert(Q::NW == T::NW && 2 * Q::TN == T::TN && 2 * Q::TM == T::TM && Q::LDS <= T::LDS, "");
+        if (!quarters) return;
+        __syncthreads();   // every wave is done with the rounds' LDS
+        int8_tiles<R8, 2, 4, 4, 2, 4, false, true>(a, Int8Tiles{tiles_m, tiles_n, total - rest, 4 * rest}, ranges, smem, bound);
+    }
 #else
     (void)a;
 #endif
@@ -348,41 +363,27 @@ __global__ __launch_bounds__(64 * WR * WC, WGS * WR * WC / 4) void int8_tile_ker
 namespace {
 
 template <bool R8, int RB, int TB, int WR, int WC, int NBUF, int WGS, bool CUT = false>
-mq_status launch_tile(const Int8Args &a, Int8Form form, Int8Part part, hipStream_t st, const Int8Ranges &ranges = {nullptr, 1}) {
+mq_status launch_tile(const Int8Args &a, Int8Form form, hipStream_t st, const Int8Ranges &ranges = {nullptr, 1}) {
     typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
     static_assert(T::TN == T::TM && (T::TM == 128 || T::TM == 256), "the forms of mq_int8_plan.h");
-    const int64_t unit = part == kInt8Quarters ? 256 : T::TM, tiles_n = cdiv(a.N, unit);
-    const int64_t tiles = int8_grid(part == kInt8Quarters ? kInt8Tile256 : form, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
+    const int64_t tiles_n = cdiv(a.N, T::TN), tiles = int8_grid(form, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
     if (tiles * ranges.splits > 0x7FFFFF00) return MQ_ERR_SHAPE;
-    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, NBUF, WGS, CUT>;
+    constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, NBUF, WGS, CUT, T::TM == 256>;
     const int lds = T::LDS + (a.offsets ? (a.E + 1) * 4 : 0);
     if (!allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
     const int64_t most = 256 * WGS;   // workgroups that fit the GPU
-    kernel<<<dim3((unsigned)std::min(part == kInt8Quarters ? most : tiles * ranges.splits, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n, part, ranges);
+    kernel<<<dim3((unsigned)std::min(tiles * ranges.splits, most)), dim3(64 * T::NW), lds, st>>>(a, (int)tiles_m, (int)tiles_n, ranges);
     return launch_status();
 }
 
 template <bool R8>
-mq_status launch_deep(const Int8Args &a, Int8Part part, hipStream_t st) {
-    return launch_tile<R8, 2, 4, 4, 2, 4, 1>(a, kInt8Deep128, part, st);
-}
-
-template <bool R8>
 mq_status launch_tiles(const Int8Args &a, Int8Form form, int splits, void *part, hipStream_t st) {
-    if (form == kInt8Deep128) {
-        if (splits == 1) return launch_deep<R8>(a, kInt8All, st);
-        const Int8Ranges ranges{static_cast<i32x4 *>(part), splits};
-        const mq_status s = launch_tile<R8, 2, 4, 4, 2, 4, 1, true>(a, form, kInt8All, st, ranges);
-        return s != MQ_OK ? s : launch_int8_join<2, 4, 4, 2>(a, ranges, st);
-    }
-    if (form == kInt8Tile128) return launch_tile<R8, 4, 4, 2, 2, 2, 2>(a, form, kInt8All, st);
-    const int64_t tiles = int8_grid(form, a.T, a.N, a.offsets ? a.E : 0, 1), rest = tiles % 256;
-    if (tiles < 256 || (!a.offsets && (rest == 0 || rest > kInt8QuarterTiles))) return launch_tile<R8, 4, 8, 4, 2, 2, 1>(a, form, kInt8All, st);
-    // (with experts the number of tiles is a bound: the launch for the rest may find nothing to do)
-    const mq_status s = launch_tile<R8, 4, 8, 4, 2, 2, 1>(a, form, kInt8Rounds, st);
-    if (s != MQ_OK) return s;
-    if (!a.offsets && rest <= kInt8DeepQuarterTiles) return launch_deep<R8>(a, kInt8Quarters, st);
-    return launch_tile<R8, 4, 4, 2, 2, 2, 2>(a, kInt8Tile128, kInt8Quarters, st);
+    if (form == kInt8Tile256) return launch_tile<R8, 4, 8, 4, 2, 2, 1>(a, form, st);
+    if (form == kInt8Tile128) return launch_tile<R8, 4, 4, 2, 2, 2, 2>(a, form, st);
+    if (splits == 1) return launch_tile<R8, 2, 4, 4, 2, 4, 1>(a, form, st);
+    const Int8Ranges ranges{static_cast<i32x4 *>(part), splits};
+    const mq_status s = launch_tile<R8, 2, 4, 4, 2, 4, 1, true>(a, form, st, ranges);
+    return s != MQ_OK ? s : launch_int8_join<2, 4, 4, 2>(a, ranges, st);
 }
 
 }  // namespace

@@ -17,7 +17,7 @@ extern "C" void int8_form(int64_t T, int64_t N, int64_t K, int64_t E, int64_t pa
     const Int8Cost &f = kInt8Costs[p.form];
     out[0] = p.form, out[1] = p.splits, out[2] = int8_grid(p.form, T, N, E, p.splits), out[3] = f.looped;
     out[4] = E == 0 ? int8_part_bytes(f, T, N, p.splits) : 0;
-    out[5] = f.places == 256 && out[2] >= 256 && out[2] % 256 != 0 && out[2] % 256 <= kInt8QuarterTiles;
+    out[5] = f.places == 256 && int8_quarters(out[2]);
     out[6] = int8_single(T, N, K, E) ? 1 + int8_single_wide(T, N, E) : 0;
 }
 extern "C" int64_t int8_part_limit(void) { return kInt8PartBytes; }

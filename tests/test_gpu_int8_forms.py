@@ -22,7 +22,7 @@ DENSE = [
     ("tile128", False, False, 4100, 5001, 144, 8, None), ("tile128", False, False, 1030, 14336, 272, 8, "silu"),
     ("tile256", False, False, 1030, 9001, 272, 8, None), ("tile256", False, False, 2050, 4352, 272, 7, "gelu"), ("tile256", False, False, 600, 14336, 16, 8, None),
     ("tile256", False, False, 3000, 9001, 144, 8, None), ("tile256", False, False, 3000, 14336, 48, 4, "silu"),
-    ("tile256", False, True, 4100, 9001, 144, 8, None), ("tile256", False, True, 4100, 9472, 144, 2, "gelu"), ("tile256", False, True, 3900, 4400, 528, 8, None),
+    ("tile256", False, True, 4100, 9001, 272, 8, None), ("tile256", False, True, 4100, 9472, 272, 2, "gelu"), ("tile256", False, True, 4100, 4099, 144, 8, None), ("tile256", False, True, 3900, 4400, 528, 8, None),
 ]
 # tokens, channels, values, whether a workgroup has 32 channels: quantized by the product's own workgroups
 SINGLE = [(1, 7, 16, False), (1, 4096, 4096, False), (2, 333, 8208, False), (3, 1027, 16384, False), (1, 14336, 1040, True), (2, 12290, 272, True), (3, 16385, 400, True)]
