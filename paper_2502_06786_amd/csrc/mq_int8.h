@@ -8,6 +8,10 @@
 namespace mq {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+// bf16 outputs side by side at any of their addresses: one store, which the memory pipeline takes apart where it has to
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
 constexpr int64_t kInt8MaxK = 131072;     // 127 * 128 * K stays below 2^31
 constexpr int64_t kMaxExperts = 1024;
@@ -155,23 +159,22 @@ __device__ __forceinline__ void store_four(const Int8Args &a, int place, int n, 
     float y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
+    // (rows of Y begin at any bf16)
     if (a.gate) {
         const uint32_t o = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
         uint16_t *out = a.Y + (int64_t)place * (a.N / 2) + n / 2;
-        if (a.N % 4 == 0) {
-            *reinterpret_cast<uint32_t *>(out) = o;
-        } else {
+        if (n + 2 < a.N)
+            *reinterpret_cast<u32_any *>(out) = o;
+        else
             out[0] = (uint16_t)o;
-            if (n + 2 < a.N) out[1] = (uint16_t)(o >> 16);
-        }
     } else {
         const u32x2 o = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
         uint16_t *out = a.Y + (int64_t)place * a.N + n;
-        if (a.N % 4 == 0) {
-            *reinterpret_cast<u32x2 *>(out) = o;
+        if (n + 3 < a.N) {
+            *reinterpret_cast<u32x2_any *>(out) = o;
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
                 if (n + e < a.N) out[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
         }
     }

@@ -168,10 +168,13 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
 
 mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const int32_t *rows, int64_t X_rows, int8_t *Xq, int64_t ldq,
                                  float *scale, int32_t *sum, hipStream_t st) {
-    // With few rows a workgroup to each, which is done sooner: 16 tokens of 4096 values 4.6 -> 3.9 us; with many the fewest lanes that hold a row.
-    if (M <= 512 && K <= 4096) return launch_tokens<256, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
-    if (M <= 256 && K <= 16384) return launch_tokens<1024, 2, 1024>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
-    if (K <= 4096) return launch_tokens<64, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    // A lane holds two to eight pieces of a row in registers.  Short rows have a wave each (11127 of 496 values 8.2 us, with room for 4096 of them 14.2;
+    // 8192 of 2048 13.4 and 15.7); a workgroup to each is done sooner where they are few or longer (600 of 4096 4.5 and 5.1 us, 16 of 4096 3.9
+    // and 4.6; 1024 threads and 256: 256 of 14336 6.2 and 6.6, 2000 of 14336 21.6 and 20.8).
+    if (K <= 1024) return launch_tokens<64, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (K <= 2048 && M > 512) return launch_tokens<64, 4, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (K <= 4096) return launch_tokens<256, 2, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
+    if (K <= 16384 && M <= 256) return launch_tokens<1024, 2, 1024>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
     if (K <= 16384) return launch_tokens<256, 8, 256>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
     return launch_tokens<1024, 16, 1024>(X, M, K, ldx, rows, X_rows, Xq, ldq, scale, sum, st);
 }

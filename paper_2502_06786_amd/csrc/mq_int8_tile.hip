@@ -208,6 +208,7 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
         uint8_t *out = smem + T::OUT + wave * 16 * T::OS;
         const int n_out = a.N >> shift, first = (t.n0 + wr * 16 * RB) >> shift;
         const int rows = t.b.count - wc * TB * 16;   // of this wave's places
+        const int last = n_out > first && n_out - first < per * 8 ? n_out % 8 : 0;   // outputs past the last whole chunk of the rows, if they are this wave's
         f32x4 ka[RB], kb[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -252,23 +253,21 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
         put();
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb, y += 16 * (int64_t)n_out) {
-            if (n_out % 8 == 0) {
-                u32x4 v[VEC];
+            u32x4 v[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = *reinterpret_cast<const u32x4 *>(out + (i * 64 + lane) / per % 16 * T::OS + (i * 64 + lane) % per * 16);
-                if (tb + 1 < TB) form(tb + 1);
+            for (int i = 0; i < VEC; ++i) v[i] = *reinterpret_cast<const u32x4 *>(out + (i * 64 + lane) / per % 16 * T::OS + (i * 64 + lane) % per * 16);
+            if (tb + 1 < TB) form(tb + 1);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const int row = (i * 64 + lane) / per, ch = (i * 64 + lane) % per;
-                    if (row < 16 && tb * 16 + row < rows && first + ch * 8 < n_out)
-                        __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4 *>(y + (int64_t)row * n_out + ch * 8));
-                }
-            } else {
-                for (int c = lane; c < min(16, rows - tb * 16) * per * 8; c += 64) {
-                    const int row = c / (per * 8), ch = c % (per * 8);
-                    if (first + ch < n_out) y[(int64_t)row * n_out + ch] = *reinterpret_cast<const uint16_t *>(out + row * T::OS + ch * 2);
-                }
-                if (tb + 1 < TB) form(tb + 1);
+            for (int i = 0; i < VEC; ++i) {
+                const int row = (i * 64 + lane) / per, ch = (i * 64 + lane) % per * 8;
+                if (row < 16 && tb * 16 + row < rows && first + ch + 8 <= n_out)
+                    __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4_any *>(y + (int64_t)row * n_out + ch));
+            }
+            if (last > 0) {
+#pragma unroll 1
+                for (int c = lane; c < 16 * 8; c += 64)
+                    if (tb * 16 + c / 8 < rows && c % 8 < last)
+                        y[(int64_t)(c / 8) * n_out + (n_out - last - first) + c % 8] = *reinterpret_cast<const uint16_t *>(out + c / 8 * T::OS + ((n_out - last - first) + c % 8) * 2);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();

@@ -43,7 +43,8 @@ def same_bits(a, b):
 
 # ---- tokens ------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("M,K,pad", [(1, 16, 0), (3, 48, 0), (65, 256, 8), (5, 4096, 0), (7, 4112, 24), (2, 16384, 0), (3, 16400, 0),
-                                     (1, 131072, 0), (300, 1008, 0), (2, 65536, 16)])
+                                     (1, 131072, 0), (300, 1008, 0), (2, 65536, 16), (513, 1024, 0), (4, 1040, 8), (513, 1040, 0), (515, 2048, 8),
+                                     (513, 2064, 0), (257, 4112, 0), (259, 16384, 0)])
 def test_tokens(mq, M, K, pad):
     x = tokens(M * 7 + K, M, K + pad)
     got = mq.mq_quantize_tokens(x.cuda()[:, :K])
