@@ -8,7 +8,8 @@ namespace mq {
 // ============================================================================================
 // A stable counting sort with E + 1 buckets, the last one for choices of no expert.  A workgroup takes kRouteChunk choices, a wave 64 of them
 // at a time.  Lanes with the same bucket find each other by comparing a bit of the bucket at a time; the first of them leaves their
-// number in count[64 choices][bucket], and sums over the earlier counts give every choice its place: no atomics, one order.
+// number in count[64 choices][bucket], and sums over the earlier counts give every choice its place: no atomics, one order.  Bound by the steps
+// that follow each other: 3.6 us for the two choices of a token, 8.5 us for 3330 of 16, 15 us in two launches for 8198 of 8.
 constexpr int kRouteThreads = 1024, kRouteSteps = 4, kRouteChunk = kRouteThreads * kRouteSteps;
 
 struct RouteArgs {
@@ -125,6 +126,7 @@ struct CombineArgs {
     int top, T;
 };
 
+// Bound by memory: 4099 tokens of 4096 outputs, two rows each, 18 us (5.6 TB/s).
 // Workgroup = up to 128 chunks of one token's row: the places and weights are the same for all its lanes.  V: values per thread, 8 where rows
 // are whole 16-byte chunks, otherwise 1.
 template <int V>

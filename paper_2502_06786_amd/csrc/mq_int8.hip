@@ -9,7 +9,9 @@ namespace mq {
 // ============================================================================================
 // quantizer of tokens
 // ============================================================================================
-// One read of the row into registers, so 2 bytes read and 1 written per value.  TPR threads to a row, V chunks of 8 values in each.
+// scale = top / 127, code = the whole number nearest to x 127 / top (ties to even).  One read of the row into registers, so 2 bytes read and 1
+// written per value, which bounds it: 8192 x 14336 64 us (5.5 TB/s; the codes fit the last-level cache), 8192 x 4096 21.7 us (4.6 TB/s); a single
+// row 2.3 us, the launch.  TPR threads to a row, V chunks of 8 values in each.
 // rows: null, or the row of X that row m of the result is made of (rows are data: whatever they hold, they stay below X_rows).
 template <int TPR, int V, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void quantize_tokens_kernel(const uint16_t *__restrict__ X, int64_t M, int K, int64_t ldx,

@@ -1,4 +1,5 @@
-// The product in 8-bit integers for few tokens: bound by the codes' way out of memory.
+// The product in 8-bit integers for few tokens: bound by the codes' way out of memory.  Every code is used by one workgroup, so LDS would only
+// add a stop on its way, and 16 channels to a workgroup give the most of them.
 #include <algorithm>
 
 #include "mq_int8.h"
@@ -73,7 +74,8 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(Int8Args a, int tiles
 }
 
 // The same on bf16 tokens, which every workgroup quantizes for itself into LDS while its first codes are on their way: up to
-// kInt8SinglePlaces places in all.  Workgroup = 16 RB channels, four waves.
+// kInt8SinglePlaces places in all.  Workgroup = 16 RB channels, four waves.  One token through 4096 x 4096 6.4 us (16.8 MB; launch, first lines
+// and the quantizer in turn are about 3.5 of them), 18432 x 2304 for each of two experts 22.8 us (85 MB).
 template <bool R8, int RB, int DEEP>
 __global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint16_t *__restrict__ X, int tiles_n, int blocks) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];   // codes [count][K + 16]
