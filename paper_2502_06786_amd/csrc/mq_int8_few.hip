@@ -74,12 +74,12 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(Int8Args a, int tiles
 }
 
 // The same on bf16 tokens, which every workgroup quantizes for itself into LDS while its first codes are on their way: up to
-// kInt8SinglePlaces places in all.  Workgroup = 16 RB channels, four waves.  One token through 4096 x 4096 6.4 us (16.8 MB; launch, first lines
-// and the quantizer in turn are about 3.5 of them), 18432 x 2304 for each of two experts 22.8 us (85 MB).
-template <bool R8, int RB, int DEEP>
-__global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint16_t *__restrict__ X, int tiles_n, int blocks) {
+// kInt8SinglePlaces places in all.  Workgroup = 16 RB channels, NW waves.  Bound by latency (launch, first lines and the quantizer in turn take about
+// 3.5 us), then by the codes: one token through 4096 x 4096 6.8 us (16.8 MB), 18432 x 2304 for each of two experts 21.8 us (85 MB).
+template <bool R8, int NW, int RB, int DEEP>
+__global__ __launch_bounds__(64 * NW) void int8_single_kernel(Int8Args a, const uint16_t *__restrict__ X, int tiles_n, int blocks) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];   // codes [count][K + 16]
-    constexpr int NW = 4, V = kInt8SingleK / (8 * 64 * NW);
+    constexpr int V = kInt8SingleK / (8 * 64 * NW);
     __shared__ i32x4 part[NW][RB][64];
     __shared__ uint32_t tops[NW];
     __shared__ int32_t sums[kInt8SinglePlaces][NW];
@@ -110,6 +110,17 @@ __global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint
 #pragma unroll
     for (int u = 0; u < DEEP; ++u) load(u, k0 + u * TURN);
 
+    // what the outputs need, requested behind the first codes
+    const int n = n0 + 16 * wave + 4 * g4;
+    float alpha[4], zero[4];
+    if (wave < RB) {
+        const int64_t first = (int64_t)b.expert * a.N;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            alpha[e] = a.alpha[first + min(n + e, a.N - 1)];
+            zero[e] = a.zero[first + min(n + e, a.N - 1)];
+        }
+    }
     const int row_bytes = a.K + 16;
     for (int j = 0; j < b.count; ++j) {
         const u32x4 *src = reinterpret_cast<const u32x4 *>(X + (int64_t)token_of(a, b.place + j) * a.K);
@@ -118,7 +129,7 @@ __global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             v[i] = u32x4{0u, 0u, 0u, 0u};
-            if ((int)(threadIdx.x + i * 256) * 8 < a.K) v[i] = src[threadIdx.x + i * 256];
+            if ((int)(threadIdx.x + i * 64 * NW) * 8 < a.K) v[i] = src[threadIdx.x + i * 64 * NW];
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) top2 = top_of(top2, v[i]);
@@ -132,7 +143,7 @@ __global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint
         int total = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int chunk = threadIdx.x + i * 256;
+            const int chunk = threadIdx.x + i * 64 * NW;
             if (chunk * 8 >= a.K) break;
             *reinterpret_cast<u32x2 *>(smem + j * row_bytes + chunk * 8) = token_codes(v[i], ts, total);
         }
@@ -162,10 +173,9 @@ __global__ __launch_bounds__(256) void int8_single_kernel(Int8Args a, const uint
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) part[wave][rb][lane] = acc[rb];
     __syncthreads();
-    const int n = n0 + 16 * wave + 4 * g4;
     if (wave >= RB || l16 >= b.count || n >= a.N) return;
     f32x4 ka, kb;
-    load_factors(a, b.expert, n, ka, kb);
+    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, a.offset, ka, kb);
     i32x4 dot = {0, 0, 0, 0};
     int total = 0;
 #pragma unroll
@@ -191,23 +201,29 @@ mq_status launch_few(const Int8Args &a, hipStream_t st) {
     return launch_status();
 }
 
-template <int RB, int DEEP>
+template <int NW, int RB, int DEEP>
 mq_status launch_single(const Int8Args &a, const uint16_t *X, hipStream_t st) {
     const int64_t tiles_n = cdiv(a.N, 16 * RB), blocks = a.offsets ? std::min(a.T, a.E) : 1;   // (an expert has one block at most)
     const int lds = a.T * (a.K + 16);
     const dim3 grid((unsigned)(tiles_n * blocks));
-    if (!(a.offset != 0.f ? allow_lds<int8_single_kernel<true, RB, DEEP>>(lds) : allow_lds<int8_single_kernel<false, RB, DEEP>>(lds))) return MQ_ERR_DEVICE;
+    if (!(a.offset != 0.f ? allow_lds<int8_single_kernel<true, NW, RB, DEEP>>(lds) : allow_lds<int8_single_kernel<false, NW, RB, DEEP>>(lds))) return MQ_ERR_DEVICE;
     if (a.offset != 0.f)
-        int8_single_kernel<true, RB, DEEP><<<grid, dim3(256), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
+        int8_single_kernel<true, NW, RB, DEEP><<<grid, dim3(64 * NW), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
     else
-        int8_single_kernel<false, RB, DEEP><<<grid, dim3(256), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
+        int8_single_kernel<false, NW, RB, DEEP><<<grid, dim3(64 * NW), lds, st>>>(a, X, (int)tiles_n, (int)blocks);
     return launch_status();
 }
 
 }  // namespace
 
+// Eight waves to 16 channels: with a workgroup or two to a compute unit four would not have enough codes on their way (4096 x 4096 7.8 -> 6.8 us,
+// 4096 x 14336 16.8 -> 15.9, 2304 x 9216 11.2 -> 10.5).  Four turns ahead where the rows are long enough and two workgroups fit a compute unit
+// (8192 x 8192 15.6 us, with two turns 16.7); with more workgroups the registers of two let three of them in (10028 x 2320 9.5 us, with four turns
+// 12.0).  With 32 channels there are several (28672 x 4096 26.4 us, with eight waves 28.2).
 mq_status launch_int8_single(const Int8Args &a, const uint16_t *X, hipStream_t st) {
-    return int8_single_wide(a.T, a.N, a.offsets ? a.E : 0) ? launch_single<2, 2>(a, X, st) : launch_single<1, 4>(a, X, st);
+    const int64_t E = a.offsets ? a.E : 0, tiles = cdiv(a.N, 16) * (E == 0 ? 1 : std::min(a.T, a.E));
+    if (int8_single_wide(a.T, a.N, E)) return launch_single<4, 2, 2>(a, X, st);
+    return tiles <= 512 && a.K > 2048 ? launch_single<8, 1, 4>(a, X, st) : launch_single<8, 1, 2>(a, X, st);
 }
 
 mq_status launch_int8_few(const Int8Args &a, hipStream_t st) { return launch_few<4, 8>(a, st); }

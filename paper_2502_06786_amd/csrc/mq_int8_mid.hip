@@ -71,6 +71,27 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = i32x4{0, 0, 0, 0};
 
+    // what the outputs need, requested before the first stage
+    float alpha[RB][4], zero[RB][4], scale[TB];
+    int sum[TB];
+    if (s.splits == 1) {
+        const int64_t first = (int64_t)b.expert * a.N;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int n = min(n0 + (wr * RB + rb) * 16 + 4 * g4 + e, a.N - 1);
+                alpha[rb][e] = a.alpha[first + n];
+                zero[rb][e] = a.zero[first + n];
+            }
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) {
+            const int m = token_of(a, b.place + min((wc * TB + tb) * 16 + l16, b.count - 1));
+            scale[tb] = a.scale[m];
+            sum[tb] = a.sum[m];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < NBUF - 1; ++i) issue(s0 + i, i);
     int buf = 0, free = NBUF - 1;
@@ -107,13 +128,12 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
     for (int rb = 0; rb < RB; ++rb) {
         const int n = n0 + (wr * RB + rb) * 16 + 4 * g4;
         f32x4 ka, kb;
-        load_factors(a, b.expert, n, ka, kb);
+        channel_factors(f32x4{alpha[rb][0], alpha[rb][1], alpha[rb][2], alpha[rb][3]}, f32x4{zero[rb][0], zero[rb][1], zero[rb][2], zero[rb][3]}, a.mult,
+                        a.offset, ka, kb);
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
             const int row = (wc * TB + tb) * 16 + l16;
-            if (row >= b.count || n >= a.N) continue;
-            const int m = token_of(a, b.place + row);
-            store_four(a, b.place + row, n, acc[rb][tb], a.scale[m], (float)a.sum[m], ka, kb);
+            if (row < b.count && n < a.N) store_four(a, b.place + row, n, acc[rb][tb], scale[tb], (float)sum[tb], ka, kb);
         }
     }
 #else

@@ -116,14 +116,16 @@ inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64
     return best;
 }
 
-// Single tokens are quantized by every workgroup of the product for itself (mq_int8_few.hip): one launch instead of two.  A token more in a
-// workgroup costs 1.2 us, the launch saved 3 to 5: one token 4096 x 4096 10.7 -> 8.2 us, 4096 x 14336 21.9 -> 17.1, two experts 2304 x 9216 19.7
-// -> 14.5; three tokens are about level, four lose (4096 x 4096 10.9 against 11.9 us).
-constexpr int kInt8SinglePlaces = 4;                    // in all; an expert may have all of them
+// Few tokens are quantized by every workgroup of the product for itself (mq_int8_few.hip): one launch instead of two.  A token more in a
+// workgroup costs 1.3 us, the launch saved 3 to 5: one token 4096 x 4096 10.7 -> 6.8 us, 4096 x 14336 21.9 -> 15.9, two experts 2304 x 9216 19.7
+// -> 15.5; with one matrix four lose (4096 x 4096 10.7 against 9.7 us).  Experts share them out: of 8, 4096 x 4096, six places 26.0 -> 20.4 us, eight 28.8
+// -> 27.2, but only where the workgroups are few and four fit a compute unit (18432 x 2304 53 -> 59 us, 2304 x 9216 40 -> 45).
+constexpr int kInt8SinglePlaces = 8;                    // in all; an expert may have all of them
 constexpr int64_t kInt8SingleK = 16384, kInt8SingleBytes = 131072;   // of a token; of all tokens, in LDS
 inline bool int8_single(int64_t T, int64_t N, int64_t K, int64_t E) {
-    const int64_t used = E == 0 ? 1 : std::min(E, T);
-    return T <= kInt8SinglePlaces && T <= 3 * used && K <= kInt8SingleK && T * (K + 16) <= kInt8SingleBytes && cdiv(N, 16) * used <= kInt8MostWorkgroups;
+    const int64_t used = E == 0 ? 1 : std::min(E, T), tiles = cdiv(N, 16) * used, bytes = T * (K + 16);
+    if (T > kInt8SinglePlaces || T > 3 * used || K > kInt8SingleK || bytes > kInt8SingleBytes || tiles > kInt8MostWorkgroups) return false;
+    return T <= 4 || (tiles <= 2048 && bytes <= 40960);
 }
 // 32 channels to a workgroup instead of 16 where that leaves three workgroups to a compute unit: 28672 x 4096 27.6 -> 26.9 us, 14336 x 4096 16.5
 // -> 15.8; below, 4096 x 4096 8.2 -> 9.5.

@@ -28,7 +28,7 @@ DENSE = [
 SINGLE = [(1, 7, 16, False), (1, 4096, 4096, False), (2, 333, 8208, False), (3, 1027, 16384, False), (1, 14336, 1040, True), (2, 12290, 272, True), (3, 16385, 400, True)]
 # form, experts, places of each (the rest have none), tokens, channels, values, bits, gate
 EXPERTS = [
-    ("few", 8, [5, 0, 0, 1, 0, 2], 7, 1027, 1040, 8, None), ("few", 40, [0] * 37 + [3, 1, 1], 4, 2304, 528, 4, "gelu"), ("few", 3, [40, 1, 49], 60, 1027, 4112, 8, None),
+    ("few", 8, [5, 0, 0, 1, 0, 3], 7, 1027, 1040, 8, None), ("few", 40, [0] * 36 + [4, 3, 1, 1], 4, 1026, 528, 4, "gelu"), ("few", 3, [40, 1, 49], 60, 1027, 4112, 8, None),
     ("mid32", 8, [3, 0, 9, 1, 0, 0, 17], 20, 9001, 528, 8, None), ("mid32", 40, [1, 2, 3] * 10 + [20, 0, 7], 50, 4098, 528, 8, "silu"), ("mid32", 8, [33, 1, 0, 64, 2, 90], 100, 9001, 4112, 2, None),
     ("mid64", 3, [100, 0, 301], 300, 2304, 2064, 8, "gelu"), ("mid64", 8, [1400, 0, 0, 0, 100, 0, 0, 0], 300, 1027, 16, 8, None),
     ("mid96", 8, [100, 1, 0, 150, 97, 0, 53], 300, 4099, 528, 8, None),
@@ -169,7 +169,8 @@ def test_experts_form(mq, case):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("E,counts,N,K", [(2, [1, 1], 2304, 2064), (8, [0, 0, 3, 0, 0, 0, 1], 520, 4112), (64, [0] * 60 + [1, 0, 2, 1], 2050, 272), (3, [0, 4, 0], 333, 1040),
-                                          (8, [1, 0, 0, 1], 18434, 144), (4, [0, 0, 0, 0], 64, 64)])
+                                          (8, [1, 0, 0, 1], 18434, 144), (4, [0, 0, 0, 0], 64, 64),
+                                          (8, [8], 1027, 1040), (3, [0, 3, 5], 2304, 2064), (64, [0] * 50 + [1, 2, 1, 0, 3], 515, 4112), (8, [1] * 8, 130, 16)])
 def test_experts_of_single_tokens(mq, E, counts, N, K):
     counts = counts + [0] * (E - len(counts))
     T = max(1, sum(counts))

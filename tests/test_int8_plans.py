@@ -38,8 +38,9 @@ def test_single_tokens_fit():
     for T, N, K, E in drawn(2000):
         f = int8_plans.form(T, N, K, E)
         if f.single:
-            # four tokens' sums, at most; codes in LDS beside the partial sums; eight chunks of eight values to each of 256 threads
-            assert T <= 4 and T * (K + 16) <= 131072 and K <= 16384
+            # eight tokens' sums, at most; codes in LDS beside the partial sums; 64 values to each of 256 threads
+            assert T <= 8 and T * (K + 16) <= 131072 and K <= 16384
     assert int8_plans.form(1, 4096, 4096).single == 1 and int8_plans.form(1, 28672, 4096).single == 2
     assert not int8_plans.form(4, 4096, 4096).single and int8_plans.form(4, 4096, 4096, 8).single
-    assert not int8_plans.form(1, 4096, 16400).single and not int8_plans.form(5, 4096, 4096, 8).single
+    assert not int8_plans.form(1, 4096, 16400).single and int8_plans.form(5, 4096, 4096, 8).single and int8_plans.form(8, 4096, 4096, 8).single
+    assert not int8_plans.form(9, 1024, 1024, 64).single and not int8_plans.form(8, 4096, 14336, 8).single and not int8_plans.form(8, 18432, 2304, 8).single
