@@ -203,7 +203,7 @@ template <int RB, int TB, int WR, int WC>
 __global__ __launch_bounds__(256) void int8_join_kernel(Int8Args a, int tiles_m, int tiles_n, Int8Ranges s) {
     constexpr int NW = WR * WC, BLOCKS = NW * RB * TB;
     const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, id = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int tile = id / BLOCKS, wave = id % BLOCKS / (RB * TB), rb = id / TB % RB, tb = id % TB, wr = wave / WC, wc = wave % WC;
+    const int tile = id / BLOCKS, wave = id % BLOCKS / (RB * TB), rb = id / TB % RB, tb = id % TB, wr = wave % WR, wc = wave / WR;
     const int tiles = tiles_m * tiles_n;
     if (tile >= tiles) return;
     const int row = tile % tiles_m * (16 * TB * WC) + (wc * TB + tb) * 16 + l16, n = tile / tiles_m * (16 * RB * WR) + (wr * RB + rb) * 16 + 4 * g4;

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
     constexpr int NW = T::NW, CL = T::TN / (8 * NW), XL = T::TM / (8 * NW), LPS = CL + XL;
     static_assert(T::TN % (8 * NW) == 0 && T::TM % (8 * NW) == 0, "");
     const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wc = wave / WR;
     const int tiles = tiles_m * tiles_n;
     const uint32_t wid = xcd_contiguous_id(blockIdx.x, gridDim.x);
     const int split = (int)(wid / (uint32_t)tiles), tile = (int)(wid % (uint32_t)tiles);
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int row = wave * 8 + (lane >> 3) + 8 * NW * i;
-        xoff[i] = (uint32_t)(token_of(a, b.place + min(row, b.count - 1)) - (int)base) * (uint32_t)a.ldq + (uint32_t)col;
+        xoff[i] = row < b.count ? (uint32_t)(token_of(a, b.place + row) - (int)base) * (uint32_t)a.ldq + (uint32_t)col : kOOB;
     }
     auto issue = [&](int st, int buf) {   // past the end of the range: out of range, zeros
         const int k0 = st * 128;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
         for (int i = 0; i < LPS; ++i) {
             const uint32_t off = i < CL ? coff + (uint32_t)i * cstep : xoff[i < CL ? 0 : i - CL];
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < CL ? rC : rX, (lds_ptr)(smem + buf * T::STAGE + (wave + i * NW) * 1024), 16,
-                                                     in ? off + (uint32_t)k0 : kOOB, 0, 0, 0);
+                                                     in ? off + (uint32_t)k0 : kOOB, 0, 0, 0);   // (kOOB + k0 is out of range too)
         }
     };
     uint32_t ca[2], xa[2];

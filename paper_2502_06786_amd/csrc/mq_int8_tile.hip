@@ -53,7 +53,7 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
     const int tiles_m = tiles.tiles_m, tiles_n = tiles.tiles_n, total = tiles.total;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g4 = lane >> 4, l16 = lane & 15, wr = wave / WC, wc = wave % WC;
+    const int g4 = lane >> 4, l16 = lane & 15, wr = wave % WR, wc = wave / WR;   // (waves i and i + 4 share a SIMD)
 
     struct Tile {
         Block b;
@@ -145,7 +145,10 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
         const int base = a.rows ? 0 : t.b.place;   // (gathered tokens lie within 2 GiB: quantize_and_multiply)
         rX = make_rsrc(a.Xq + (int64_t)base * a.ldq, (uint64_t)(a.M - base) * a.ldq);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)(min(max(tokens[i], 0), a.M - 1) - base) * (uint32_t)a.ldq + (uint32_t)col;
+        for (int i = 0; i < XL; ++i) {   // rows past the block's places: out of range, zeros, which cost neither memory nor much power
+            const int row = wave * 8 + (here(lane) >> 3) + 8 * NW * i;
+            xoff[i] = row < t.b.count ? (uint32_t)(min(max(tokens[i], 0), a.M - 1) - base) * (uint32_t)a.ldq + (uint32_t)col : kOOB;
+        }
         uint8_t *to = smem + T::PARAMS + set * T::PARAM_SET + wave * 512;
         const void *one, *two;
         if (wave < T::TN / 64) {
@@ -314,6 +317,15 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
             k0 += 128;
             buf = buf + 1 == NBUF ? 0 : buf + 1;
         };
+        if (WC > 1 && cur.b.count <= wc * TB * 16) {   // no places for this wave: it only fetches, and leaves its SIMD to the other one.
+            // (Both: 8 experts of 1025 tokens, 28672 x 4096, 1070 -> 1036 us; 300 tokens through 14336 x 4096 28.3 -> 27.6)
+            for (; k0 < k_end; k0 += 128) {
+                stage_barrier<(NBUF - 2) * LPS, 0>();
+#pragma unroll
+                for (int i = 0; i < LPS; ++i) issue_one(std::false_type{}, k0 + 128 * NBUF, buf, i);
+                buf = buf + 1 == NBUF ? 0 : buf + 1;
+            }
+        }
         while (k0 + 128 * (NBUF + 1) <= k_end) stage(std::true_type{});
         while (k0 < k_end) stage(std::false_type{});
         mfma16_settle();
