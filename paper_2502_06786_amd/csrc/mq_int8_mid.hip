@@ -1,7 +1,7 @@
 // The product in 8-bit integers between few and many tokens: small tiles through LDS, several workgroups to a compute unit, K split over
 // workgroups where there are not enough tiles.  Bound by memory: three stages of 64 rows of codes and the tokens' (12 to 20 KB each) are on their
-// way per workgroup, two or three of those to a compute unit, 36 to 60 KB times that.  16 tokens through 28672 x 4096 26.9 us (4.4 TB/s), 23 to each
-// of 8 experts of that size 175 us (5.5 TB/s), 77 through 4096 x 14336 in four ranges 15.7 us and 4 for their sum.  Codes straight to registers
+// way per workgroup, two or three of those to a compute unit, 36 to 60 KB times that.  16 tokens through 28672 x 4096 26.7 us (4.4 TB/s), 23 to each
+// of 8 experts of that size 174 us (5.5 TB/s), 77 through 4096 x 14336 in four ranges 15.7 us and 4 for their sum.  Codes straight to registers
 // were slower (every wave waits for its own).
 #include "mq_int8.h"
 #include "mq_linear.h"

@@ -1,5 +1,5 @@
-// The product in 8-bit integers for many tokens: tiles through LDS.  Bound by the matrix core and its power: 8192 x 28672 x 3584 with a gate 704 us
-// (2.39 POP/s; the core is busy 62 % of the cycles at 1.7 GHz), 2011 x 14336 x 4096 83 us (2.85 POP/s before the clock goes down).  A tile's
+// The product in 8-bit integers for many tokens: tiles through LDS.  Bound by the matrix core and its power: 8192 x 28672 x 3584 with a gate 700 us
+// (2.40 POP/s; the core is busy 61 % of the cycles at 1.7 GHz), 2011 x 14336 x 4096 83 us (2.85 POP/s before the clock goes down).  A tile's
 // operands come through LDS once per wave that needs them: 64 x 128 per wave reads 24 KB for 128 products of 16 cycles.  What counted:
 // stages of 128 k, whose rows are whole lines of the L2 (64 k: 8 % slower); products without a pause, operands of the next half replaced behind
 // the last product that uses them; the next tile's first stages on their way, and nothing spilled, while outputs are formed; those through LDS to
