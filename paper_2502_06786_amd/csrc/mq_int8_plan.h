@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "mq_plan.h"
 
@@ -20,26 +21,27 @@ enum Int8Form { kInt8Few, kInt8Mid32, kInt8Mid64, kInt8Mid96, kInt8Deep128, kInt
 // them share it; `end` is what a tile costs besides its stages, `launch` what a call does; codes and tokens arrive at `bytes_us` bytes in
 // a us at most (the large tiles hold two stages: they wait for memory longer), and ranges of K cost `join` and the traffic of their
 // partial sums.  Fitted to 5600 times (13 layers from 6000 x 512 to 28672 x 4096, 1 to 4096 tokens, 1 to 16 ranges; replayed from a graph; root mean
-// square of the misfit 5 to 12 %): of the forms and ranges timed at 259 sizes, the one that the rule takes is 3 % slower than the best on
-// average, 25 % at worst.
+// square of the misfit 5 to 12 %): of the forms and ranges timed at 259 sizes, the one that the rule takes is 2 % slower than the best on
+// average, 16 % at worst.
 struct Int8Cost {
     int channels, places, per_cu;
     bool looped;
     double launch, end, alone, full, bytes_us, join, join_bytes_us;
 };
 constexpr Int8Cost kInt8Costs[kInt8Forms] = {
-    {16, 16, 3, false, 0.57, 2.48, 0.079, 0.216, 5.3e6, 0, 1},
-    {64, 32, 3, false, 2.38, 1.29, 0.182, 0.438, 5.3e6, 2.01, 7.8e6},
-    {64, 64, 2, false, 2.92, 1.23, 0.251, 0.484, 5.3e6, 1.50, 7.3e6},
-    {64, 96, 2, false, 3.41, 1.37, 0.335, 0.614, 5.2e6, 1.21, 7.1e6},
+    {16, 16, 3, false, 0.16, 2.89, 0.079, 0.207, 5.3e6, 0, 1},
+    {64, 32, 3, false, 2.23, 1.37, 0.183, 0.422, 5.3e6, 2.00, 7.6e6},
+    {64, 64, 2, false, 2.50, 1.57, 0.252, 0.459, 5.3e6, 1.57, 7.6e6},
+    {64, 96, 2, false, 3.07, 1.58, 0.339, 0.556, 5.3e6, 1.05, 6.7e6},
     {128, 128, 1, true, 2.76, 2.94, 0.319, 0.487, 5.3e6, 1.98, 6.5e6},
     {128, 128, 2, true, 0.0, 3.94, 0.601, 0.823, 3.2e6, 0, 1},
     {256, 256, 1, true, 0.0, 7.57, 1.033, 1.033, 2.25e6, 0, 1},
 };
+constexpr double kInt8Uneven = 0.7;
 constexpr double kInt8TokensUs = 14e6;   // bytes of tokens that the FEW form's workgroups read from the L2s in a us
 // Products by expert (105 times of 8 to 64 experts with 8 to 125 tokens each): finding its block costs a workgroup `kInt8FindUs` (one that loops
 // over tiles keeps the experts' bounds); codes that few tiles share come late, which a stage feels (`kInt8ExpertStage` times as long), while
-// the tiles with two stages get more bytes in a us than from one matrix (`kInt8ExpertBytes` times).  The form taken is 2 % slower than the best on
+// the tiles with two stages get more bytes in a us than from one matrix (`kInt8ExpertBytes` times).  The form taken is 1 % slower than the best on
 // average, 12 % at worst.
 constexpr double kInt8FindUs = 2.5, kInt8ExpertStage = 1.6, kInt8ExpertBytes = 1.5;
 
@@ -74,8 +76,9 @@ inline double int8_cost(int form, int64_t T, int64_t N, int64_t K, int64_t E, in
         t = rounds * (stages * f.full + f.end) + last + (E ? kInt8FindUs : 0.0);
         if (E && form != kInt8Deep128) rate *= kInt8ExpertBytes;
     } else {
-        const double share = tiles / 256.0;
-        t = std::max(stages * f.alone, stages * f.full / f.per_cu * share) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
+        // (some compute units have a workgroup more than their share; with experts the number of tiles is not known that well)
+        const double share = tiles / 256.0, most = E ? share : share + kInt8Uneven * (std::ceil(share) - share);
+        t = std::max(stages * f.alone, stages * f.full / f.per_cu * most) + (f.end + (E ? kInt8FindUs : 0.0)) * std::max(1.0, share / f.per_cu);
     }
     t = std::max(t, (used * (double)N * (double)K + (double)T * (double)K) / rate);
     if (form == kInt8Few) t += tiles * (double)std::min<int64_t>(T, 16) * (double)K / kInt8TokensUs;

@@ -11,10 +11,10 @@ from tests import int8_plans, int8_reference as ref
 DENSE = [
     ("few", False, False, 16, 333, 1040, 8, None), ("few", False, False, 9, 1028, 2064, 4, "silu"), ("few", False, False, 5, 4099, 4112, 8, None),
     ("mid32", False, False, 50, 4099, 528, 8, None), ("mid32", False, False, 70, 2304, 1040, 4, "gelu"), ("mid32", False, False, 33, 5001, 16, 8, None),
-    ("mid32", True, False, 33, 2051, 4112, 8, None), ("mid32", True, False, 30, 4352, 4112, 2, "silu"), ("mid32", True, False, 13, 70, 8208, 8, None),
-    ("mid64", False, False, 511, 4099, 272, 8, None), ("mid64", False, False, 180, 9472, 528, 6, "gelu"),
+    ("mid32", True, False, 20, 2051, 4112, 8, None), ("mid32", True, False, 30, 4352, 4112, 2, "silu"), ("mid32", True, False, 13, 70, 8208, 8, None),
+    ("mid64", False, False, 401, 4099, 528, 8, None), ("mid64", False, False, 180, 9472, 528, 6, "gelu"),
     ("mid64", True, False, 100, 2050, 4112, 8, "gelu"), ("mid64", True, False, 300, 1027, 4112, 3, None),
-    ("mid96", False, False, 180, 9001, 2064, 8, None), ("mid96", False, False, 770, 9472, 16, 5, "silu"),
+    ("mid96", False, False, 600, 2051, 4112, 8, None), ("mid96", False, False, 200, 5002, 4112, 5, "silu"),
     ("mid96", True, False, 180, 4352, 8208, 4, "silu"), ("mid96", True, False, 77, 4099, 8208, 8, None),
     ("deep128", False, False, 511, 4099, 1040, 8, None), ("deep128", False, False, 200, 9472, 1040, 4, "gelu"), ("deep128", False, False, 401, 5001, 1040, 8, None),
     ("deep128", True, False, 770, 1027, 8208, 8, None), ("deep128", True, False, 200, 4352, 8208, 6, "silu"), ("deep128", True, False, 255, 4099, 8208, 2, None),
@@ -32,7 +32,7 @@ EXPERTS = [
     ("mid32", 8, [3, 0, 9, 1, 0, 0, 17], 20, 9001, 528, 8, None), ("mid32", 40, [1, 2, 3] * 10 + [20, 0, 7], 50, 4098, 528, 8, "silu"), ("mid32", 8, [33, 1, 0, 64, 2, 90], 100, 9001, 4112, 2, None),
     ("mid64", 3, [100, 0, 301], 300, 2304, 2064, 8, "gelu"), ("mid64", 8, [1400, 0, 0, 0, 100, 0, 0, 0], 300, 1027, 16, 8, None),
     ("mid96", 8, [100, 1, 0, 150, 97, 0, 53], 300, 4099, 528, 8, None),
-    ("deep128", 3, [128, 640, 2], 500, 2304, 4112, 8, "silu"), ("deep128", 8, [1, 127, 129, 0, 0, 256, 257, 0], 333, 2304, 528, 8, None),
+    ("deep128", 3, [128, 640, 2], 500, 2304, 4112, 8, "silu"), ("deep128", 8, [1, 127, 129, 0, 0, 256, 257, 1], 333, 2304, 1040, 8, None),
     ("tile128", 3, [1000, 1, 499], 500, 4352, 144, 8, "silu"), ("tile128", 40, [150] * 40, 2000, 9001, 144, 4, None),
     ("tile256", 8, [300, 0, 1, 600, 255, 256, 88, 0], 1000, 4099, 528, 8, None), ("tile256", 3, [2000, 4000, 0], 5000, 2304, 144, 8, "gelu"),
     ("tile256", 3, [1, 5998, 1], 3000, 9002, 144, 8, "silu"), ("tile256", 8, [3000, 0, 2, 0, 0, 1480, 1, 1517], 3000, 9001, 144, 4, None),
