@@ -496,7 +496,7 @@ mq_status mq_linear_bwd_gated(const uint16_t *X, const uint8_t *Q, const float *
  *   flags  0, or MQ_FLAG_GATED, with MQ_FLAG_FFN_SILU or without it: the layer is a stacked gate / up layer (channels 2 f and
  *          2 f + 1 are a pair, as in mq_linear_fwd_multi_gated, N even) and Y [M, N / 2] receives
  *          bf16(act(y_2f) * y_2f+1) of the fp32 outputs y, act = SiLU with MQ_FLAG_FFN_SILU, otherwise GELU in its tanh form.
- *          Any other flag is refused (MQ_ERR_BITS)
+ *          Any other flag, and MQ_FLAG_FFN_SILU alone, is refused (MQ_ERR_BITS)
  *   Y      [M, N] bf16 out (with MQ_FLAG_GATED [M, N / 2]); may not overlap an input
  *   ws     workspace of at least mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1)
  * K a multiple of 16, K <= 131072; M and N are free below 2^31 - 256.  M == 0 or N == 0 is a no-op.

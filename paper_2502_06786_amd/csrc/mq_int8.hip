@@ -113,7 +113,7 @@ mq_status launch_int8(const Int8Args &a, void *part, size_t part_bytes, hipStrea
 mq_status check_int8(int64_t M, int64_t N, int64_t K, int r, uint32_t flags) {
     if (M < 0 || N < 0 || K < 1 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > kInt8MaxK) return MQ_ERR_SHAPE;
     if (r < 1 || r > 8) return MQ_ERR_BITS;
-    if (flags & ~(uint32_t)(MQ_FLAG_GATED | MQ_FLAG_FFN_SILU)) return MQ_ERR_BITS;
+    if ((flags & ~(uint32_t)(MQ_FLAG_GATED | MQ_FLAG_FFN_SILU)) || flags == MQ_FLAG_FFN_SILU) return MQ_ERR_BITS;
     if (K % 16 != 0 || ((flags & MQ_FLAG_GATED) && N % 2 != 0)) return MQ_ERR_ALIGN;
     return MQ_OK;
 }

@@ -1,0 +1,23 @@
+"""What the C calls of the layer in 8-bit integers refuse before their first launch, beside tests/test_int8_abi.py (no GPU: nothing is
+enqueued by a call that fails, so none is needed)."""
+from tests.test_int8_abi import ALIGN, BITS, GATED, P, SILU, lib  # noqa: F401 (lib is a fixture)
+
+
+def linear(lib, M=4, N=32, K=64, r=8, flags=0, ws=P, ws_bytes=1 << 62):  # noqa: F811
+    return lib.mq_linear_fwd_int8(P, P, P, P, M, N, K, r, flags, P, ws, ws_bytes, None)
+
+
+def quantized(lib, M=4, N=32, K=64, r=8, flags=0, ws=None, ws_bytes=0):  # noqa: F811
+    return lib.mq_linear_fwd_int8_quantized(P, P, P, P, P, P, M, N, K, r, flags, P, ws, ws_bytes, None)
+
+
+def experts(lib, M=8, rows=P, T=16, E=4, N=32, K=64, r=8, flags=0, ws=P, ws_bytes=1 << 62):  # noqa: F811
+    return lib.mq_experts_fwd_int8(P, M, rows, P, P, P, P, T, E, N, K, r, flags, P, ws, ws_bytes, None)
+
+
+def test_the_kind_of_gate_without_a_gate(lib):  # noqa: F811
+    """SiLU says which gate; alone it would be a product without one, whose Y is twice as wide as that of the caller who forgot the other flag."""
+    for call in (linear, quantized, experts):
+        assert call(lib, flags=SILU) == BITS
+        assert call(lib, flags=SILU, N=31) == BITS
+        assert call(lib, flags=SILU | GATED, N=31) == ALIGN   # the pair is a gate: refused for the odd number of channels only
