@@ -45,18 +45,21 @@ __device__ __forceinline__ i32x4 mfma_i8(const i32x4 &a, const i32x4 &b, const i
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-// scale (alpha 2^(8-r) dot - alpha (zero - offset) sum): the same fp32 steps in every kernel, and `dot` is a sum of whole numbers, so the
-// outputs of all forms of the product are the same bits.  (dot and sum below 2^31 are rounded to fp32: 2^-24 of terms that the
-// centring keeps near the size of the result.)  The token's scale last: it may be as small as a bf16 subnormal / 127.
-__device__ __forceinline__ void channel_factors(const f32x4 &alpha, const f32x4 &zero, float mult, float offset, f32x4 &ka, f32x4 &kb) {
+// scale (alpha 2^(8-r) (dot + offset sum) - alpha zero sum): the same fp32 steps in every kernel, and `dot` is a sum of whole numbers, so the
+// outputs of all forms of the product are the same bits.  (dot below 2^31 and dot + offset sum are rounded to fp32: 2^-24 of themselves.)
+// The offset goes back to the sum and not into the zero-point: a channel whose weights are all w has codes of 0 and zero = -w, dot + offset sum is
+// then 0 to the last bit, while zero - offset loses what is small beside 128 (w = 3e-5 came out 5 % off).  One instruction more per
+// output: 8192 x 28672 x 3584 with a gate 723 -> 725 us, the shorter calls within their spread.  The token's scale last: it may be as small as
+// a bf16 subnormal / 127.
+__device__ __forceinline__ void channel_factors(const f32x4 &alpha, const f32x4 &zero, float mult, f32x4 &ka, f32x4 &kb) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         ka[e] = alpha[e] * mult;
-        kb[e] = alpha[e] * (zero[e] - offset);
+        kb[e] = alpha[e] * zero[e];
     }
 }
-__device__ __forceinline__ float int8_output(int dot, float sum, float scale, float ka, float kb) {
-    return __builtin_fmaf(ka, (float)dot, -(kb * sum)) * scale;
+__device__ __forceinline__ float int8_output(int dot, float sum, float scale, float ka, float kb, float offset) {
+    return __builtin_fmaf(ka, __builtin_fmaf(offset, sum, (float)dot), -(kb * sum)) * scale;
 }
 
 // act(g) u, act(v) = v / (1 + exp(-t)): t = v for SiLU, 2 sqrt(2 / pi) (v + 0.044715 v^3) for GELU in its tanh form.  The gate acts on
@@ -158,7 +161,7 @@ __device__ __forceinline__ void store_four(const Int8Args &a, int place, int n, 
                                            const f32x4 &kb) {
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e]);
+    for (int e = 0; e < 4; ++e) y[e] = int8_output(dot[e], sum, scale, ka[e], kb[e], a.offset);
     // (rows of Y begin at any bf16)
     if (a.gate) {
         const uint32_t o = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
@@ -188,7 +191,7 @@ __device__ __forceinline__ void load_factors(const Int8Args &a, int expert, int 
         al[e] = alpha[min(n + e, a.N - 1)];
         ze[e] = zero[min(n + e, a.N - 1)];
     }
-    channel_factors(al, ze, a.mult, a.offset, ka, kb);
+    channel_factors(al, ze, a.mult, ka, kb);
 }
 
 // ---- ranges of K ------------------------------------------------------------------------------------------

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * NW) void int8_few_kernel(Int8Args a, int tiles
     __syncthreads();
     if (wave > 0 || l16 >= b.count || n >= a.N) return;
     f32x4 ka, kb;
-    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, a.offset, ka, kb);
+    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, ka, kb);
 #pragma unroll
     for (int w = 1; w < NW; ++w) acc += part[w][lane];
     store_four(a, b.place + l16, n, acc, scale, (float)total, ka, kb);
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * NW) void int8_single_kernel(Int8Args a, const 
     __syncthreads();
     if (wave >= RB || l16 >= b.count || n >= a.N) return;
     f32x4 ka, kb;
-    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, a.offset, ka, kb);
+    channel_factors(f32x4{alpha[0], alpha[1], alpha[2], alpha[3]}, f32x4{zero[0], zero[1], zero[2], zero[3]}, a.mult, ka, kb);
     i32x4 dot = {0, 0, 0, 0};
     int total = 0;
 #pragma unroll

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_mid_kernel(Int8Args a, int 
         const int n = n0 + (wr * RB + rb) * 16 + 4 * g4;
         f32x4 ka, kb;
         channel_factors(f32x4{alpha[rb][0], alpha[rb][1], alpha[rb][2], alpha[rb][3]}, f32x4{zero[rb][0], zero[rb][1], zero[rb][2], zero[rb][3]}, a.mult,
-                        a.offset, ka, kb);
+                        ka, kb);
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
             const int row = (wc * TB + tb) * 16 + l16;

@@ -222,7 +222,7 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
         for (int rb = 0; rb < RB; ++rb) {
             const int n = (wr * RB + rb) * 16 + 4 * g4;
             const uint8_t *at = params + (n >> 6) * 512 + (n & 63) * 4;
-            channel_factors(*reinterpret_cast<const f32x4 *>(at), *reinterpret_cast<const f32x4 *>(at + 256), a.mult, a.offset, ka[rb], kb[rb]);
+            channel_factors(*reinterpret_cast<const f32x4 *>(at), *reinterpret_cast<const f32x4 *>(at + 256), a.mult, ka[rb], kb[rb]);
         }
         float scale[TB], sum[TB];
 #pragma unroll
@@ -238,7 +238,7 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
             for (int rb = 0; rb < RB; ++rb) {
                 float y[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum[tb], scale[tb], ka[rb][e], kb[rb][e]);
+                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum[tb], scale[tb], ka[rb][e], kb[rb][e], a.offset);
                 if constexpr (GATED)
                     o[rb][0] = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
                 else
