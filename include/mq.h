@@ -499,7 +499,7 @@ mq_status mq_linear_bwd_gated(const uint16_t *X, const uint8_t *Q, const float *
  *          Any other flag, and MQ_FLAG_FFN_SILU alone, is refused (MQ_ERR_BITS)
  *   Y      [M, N] bf16 out (with MQ_FLAG_GATED [M, N / 2]); may not overlap an input
  *   ws     workspace of at least mq_workspace_bytes(MQ_OP_LINEAR_FWD_INT8, M, N, K, 1)
- * K a multiple of 16, K <= 131072; M and N are free below 2^31 - 256.  M == 0 or N == 0 is a no-op.
+ * K a multiple of 16, K <= 131072; M and N are free below 2^31 - 256, M * N below 2^45 or so (2^31 tiles).  M == 0 or N == 0 is a no-op.
  * With few tokens K may be cut into ranges whose partial sums (64 MiB at most) go through the workspace.  One that holds the tokens
  * but not these (made for other sizes of the layer) is accepted: K is then not cut, which is slower; the results' bits are the same.
  * mq_linear_fwd_int8_quantized: the same on tokens that mq_quantize_tokens has quantized (several layers on one input).  ws may be

@@ -93,13 +93,12 @@ Int8Layout int8_layout(int64_t M, int64_t K) {
     l.part = off;
     return l;
 }
-Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64_t part_bytes) {
-    return remembered<Int8Plan>(make_int8_plan, T, N, K, E, std::min(part_bytes, kInt8PartBytes));
+Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, size_t part_bytes) {
+    return remembered<Int8Plan>(make_int8_plan, T, N, K, E, (int64_t)std::min(part_bytes, (size_t)kInt8PartBytes));
 }
 
-// `part`: room of part_bytes for partial sums, 256-byte aligned
-mq_status launch_int8(const Int8Args &a, void *part, size_t part_bytes, hipStream_t st) {
-    const Int8Plan plan = int8_plan(a.T, a.N, a.K, a.offsets ? a.E : 0, (int64_t)std::min<size_t>(part_bytes, (size_t)kInt8PartBytes));
+// `part`: room for the partial sums of the plan's ranges, 256-byte aligned
+mq_status launch_int8(const Int8Args &a, const Int8Plan &plan, void *part, hipStream_t st) {
     switch (plan.form) {
         case kInt8Few: return launch_int8_few(a, st);
         case kInt8Mid32: return launch_int8_mid(a, 32, plan.splits, part, st);
@@ -146,7 +145,10 @@ Int8Args int8_args(const uint8_t *codes, const float *alpha, const float *zero, 
 mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t ws_bytes, hipStream_t st) {
     const Int8Layout l = int8_layout(a.M > a.T ? a.M : a.T, a.K);
     if (!ws || !aligned16(ws) || ws_bytes < l.part + 256) return MQ_ERR_WORKSPACE;
-    if (int8_single(a.T, a.N, a.K, a.offsets ? a.E : 0)) return launch_int8_single(a, X, st);
+    const int64_t E = a.offsets ? a.E : 0;
+    if (int8_single(a.T, a.N, a.K, E)) return launch_int8_single(a, X, st);
+    const Int8Plan plan = int8_plan(a.T, a.N, a.K, E, ws_bytes - l.part - 256);
+    if (!int8_launches(plan, a.T, a.N, E)) return MQ_ERR_SHAPE;
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
     int8_t *Xq = reinterpret_cast<int8_t *>(base + l.codes);
     a.ldq = (int)(cdiv(a.K, kInt8Line) * kInt8Line);
@@ -163,7 +165,7 @@ mq_status quantize_and_multiply(Int8Args a, const uint16_t *X, void *ws, size_t 
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
-    return launch_int8(a, base + l.part, ws_bytes - l.part - 256, st);
+    return launch_int8(a, plan, base + l.part, st);
 }
 
 }  // namespace
@@ -219,8 +221,10 @@ extern "C" mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float 
     a.Xq = Xq;
     a.scale = scale;
     a.sum = sum;
+    const Int8Plan plan = int8_plan(M, N, K, 0, ws && ws_bytes > 256 ? ws_bytes - 256 : 0);
+    if (!int8_launches(plan, M, N, 0)) return MQ_ERR_SHAPE;
     uint8_t *part = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-    return launch_int8(a, part, ws && ws_bytes > 256 ? ws_bytes - 256 : 0, static_cast<hipStream_t>(hip_stream));
+    return launch_int8(a, plan, part, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" mq_status mq_linear_fwd_int8(const uint16_t *X, const uint8_t *codes, const float *alpha, const float *zero, int64_t M, int64_t N,

@@ -191,7 +191,6 @@ namespace {
 template <int NW, int DEEP>
 mq_status launch_few(const Int8Args &a, hipStream_t st) {
     const int64_t tiles_n = cdiv(a.N, 16), grid_size = int8_grid(kInt8Few, a.T, a.N, a.offsets ? a.E : 0, 1), blocks = grid_size / tiles_n;
-    if (grid_size > kInt8MostWorkgroups) return MQ_ERR_SHAPE;
     const dim3 grid((unsigned)grid_size), threads(64 * NW);
     static_assert(NW <= 4, "");
     if (a.offset != 0.f)

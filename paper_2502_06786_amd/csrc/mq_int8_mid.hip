@@ -148,7 +148,6 @@ mq_status launch_mid(const Int8Args &a, int splits, void *part, hipStream_t st) 
     typedef Int8Mid<RB, TB, WR, WC, NBUF> T;
     const int64_t tiles_n = cdiv(a.N, T::TN), grid = int8_grid(T::TM == 32 ? kInt8Mid32 : T::TM == 64 ? kInt8Mid64 : kInt8Mid96, a.T, a.N, a.offsets ? a.E : 0, splits);
     const int64_t tiles_m = grid / tiles_n / splits;
-    if (grid > kInt8MostWorkgroups) return MQ_ERR_SHAPE;
     static_assert(T::NW <= 4 && T::TN == 64 && (T::TM == 32 || T::TM == 64 || T::TM == 96), "the forms of mq_int8_plan.h");
     constexpr auto kernel = int8_mid_kernel<R8, RB, TB, WR, WC, NBUF>;
     if (!allow_lds<kernel>(T::LDS)) return MQ_ERR_DEVICE;

@@ -94,6 +94,7 @@ inline int64_t int8_grid(int form, int64_t T, int64_t N, int64_t E, int splits) 
 }
 // (a launch has less than 2^32 threads)
 constexpr int64_t kInt8MostWorkgroups = 0xFFFFFF;   // of 256 threads
+constexpr int64_t kInt8MostTiles = 0x7FFFFC00;      // where they are looped over: an id past the last one, up to 512 further, still fits 32 bits
 
 struct Int8Plan {
     int form, splits;
@@ -117,6 +118,11 @@ inline Int8Plan make_int8_plan(int64_t T, int64_t N, int64_t K, int64_t E, int64
         }
     }
     return best;
+}
+
+// (calls of 2^45 outputs and more do not)
+inline bool int8_launches(const Int8Plan &p, int64_t T, int64_t N, int64_t E) {
+    return int8_grid(p.form, T, N, E, p.splits) <= (kInt8Costs[p.form].looped ? kInt8MostTiles : kInt8MostWorkgroups);
 }
 
 // Few tokens are quantized by every workgroup of the product for itself (mq_int8_few.hip): one launch instead of two.  A token more in a

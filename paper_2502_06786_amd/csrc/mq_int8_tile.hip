@@ -384,7 +384,6 @@ mq_status launch_tile(const Int8Args &a, Int8Form form, hipStream_t st, const In
     typedef Int8Tile<RB, TB, WR, WC, NBUF> T;
     static_assert(T::TN == T::TM && (T::TM == 128 || T::TM == 256), "the forms of mq_int8_plan.h");
     const int64_t tiles_n = cdiv(a.N, T::TN), tiles = int8_grid(form, a.T, a.N, a.offsets ? a.E : 0, 1), tiles_m = tiles / tiles_n;
-    if (tiles * ranges.splits > 0x7FFFFF00) return MQ_ERR_SHAPE;
     constexpr auto kernel = int8_tile_kernel<R8, RB, TB, WR, WC, NBUF, WGS, CUT, T::TM == 256>;
     const int lds = T::LDS + (a.offsets ? (a.E + 1) * 4 : 0);
     if (!allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;

@@ -1,6 +1,6 @@
 """What the C calls of the layer in 8-bit integers refuse before their first launch, beside tests/test_int8_abi.py (no GPU: nothing is
 enqueued by a call that fails, so none is needed)."""
-from tests.test_int8_abi import ALIGN, BITS, GATED, P, SILU, lib  # noqa: F401 (lib is a fixture)
+from tests.test_int8_abi import ALIGN, BITS, GATED, P, SHAPE, SILU, lib  # noqa: F401 (lib is a fixture)
 
 
 def linear(lib, M=4, N=32, K=64, r=8, flags=0, ws=P, ws_bytes=1 << 62):  # noqa: F811
@@ -21,3 +21,13 @@ def test_the_kind_of_gate_without_a_gate(lib):  # noqa: F811
         assert call(lib, flags=SILU) == BITS
         assert call(lib, flags=SILU, N=31) == BITS
         assert call(lib, flags=SILU | GATED, N=31) == ALIGN   # the pair is a gate: refused for the odd number of channels only
+
+
+def test_more_tiles_than_a_launch_counts(lib):  # noqa: F811
+    """2^45 outputs and more: refused like any other size, before the tokens are quantized (that launch would come back as DEVICE here)."""
+    most = 0x7FFFFF00
+    for call in (linear, quantized):
+        assert call(lib, M=most, N=most, K=16) == SHAPE
+        assert call(lib, M=1 << 24, N=1 << 24, K=4096) == SHAPE
+    assert experts(lib, M=most, T=most, E=1024, N=most, K=16) == SHAPE
+    assert experts(lib, M=1, T=1 << 20, E=1024, N=most, K=16) == SHAPE
