@@ -197,7 +197,7 @@ mq_status launch_route(const RouteArgs &a, hipStream_t st) {
 }  // namespace
 
 size_t route_workspace_bytes(int64_t n, int64_t E) {
-    if (E < 1 || E > kMaxExperts || n > 0x7FFFFF00) return 0;
+    if (E < 1 || E > kMaxExperts || n < 0 || n > 0x7FFFFF00) return 0;
     return (size_t)cdiv(n, kRouteChunk) * (size_t)(E + 1) * 4 + 256;
 }
 

@@ -109,8 +109,9 @@ mq_status launch_int8(const Int8Args &a, const Int8Plan &plan, void *part, hipSt
 }
 
 // sizes, bits and flags of a product
+bool int8_sizes(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 0 && K >= 1 && M <= 0x7FFFFF00 && N <= 0x7FFFFF00 && K <= kInt8MaxK; }
 mq_status check_int8(int64_t M, int64_t N, int64_t K, int r, uint32_t flags) {
-    if (M < 0 || N < 0 || K < 1 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > kInt8MaxK) return MQ_ERR_SHAPE;
+    if (!int8_sizes(M, N, K)) return MQ_ERR_SHAPE;
     if (r < 1 || r > 8) return MQ_ERR_BITS;
     if ((flags & ~(uint32_t)(MQ_FLAG_GATED | MQ_FLAG_FFN_SILU)) || flags == MQ_FLAG_FFN_SILU) return MQ_ERR_BITS;
     if (K % 16 != 0 || ((flags & MQ_FLAG_GATED) && N % 2 != 0)) return MQ_ERR_ALIGN;
@@ -184,7 +185,7 @@ mq_status launch_quantize_tokens(const uint16_t *X, int64_t M, int64_t K, int64_
 }
 
 size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K, bool grouped) {
-    if (K < 1 || K > kInt8MaxK) return 0;
+    if (!int8_sizes(M, N, K) || K % 16 != 0) return 0;
     size_t part = 0;
     if (!grouped && M > 0 && N > 0) {
         const Int8Plan plan = int8_plan(M, N, K, 0, kInt8PartBytes);

@@ -31,3 +31,15 @@ def test_more_tiles_than_a_launch_counts(lib):  # noqa: F811
         assert call(lib, M=1 << 24, N=1 << 24, K=4096) == SHAPE
     assert experts(lib, M=most, T=most, E=1024, N=most, K=16) == SHAPE
     assert experts(lib, M=1, T=1 << 20, E=1024, N=most, K=16) == SHAPE
+
+
+def test_workspaces_of_sizes_that_the_calls_refuse(lib):  # noqa: F811
+    """0, as for other invalid arguments, and not what is left of a product that does not fit 64 bits."""
+    f, most = lib.mq_workspace_bytes, 0x7FFFFF00
+    for op in (8, 10):
+        assert f(op, most, 64, 16, 1) > most * 128 and f(op, 4, most, 16, 1) > 0
+        assert f(op, most + 1, 64, 16, 1) == f(op, 4, most + 1, 16, 1) == 0
+        assert f(op, 1 << 57, 64, 16, 1) == f(op, 1 << 62, 1 << 62, 131072, 1) == 0
+        assert f(op, 4, 64, 72, 1) == 0
+    assert f(9, most + 1, 64, 0, 1) == f(9, -1, 64, 0, 1) == 0
+    assert f(9, 5000, 64, -1, 1) == f(9, 5000, 64, 0, 1) > 0   # (K is not looked at)
