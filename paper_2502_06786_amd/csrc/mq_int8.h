@@ -3,6 +3,7 @@
 #pragma once
 
 #include "mq_gemv.h"
+#include "mq_int8_blocks.h"
 #include "mq_int8_plan.h"
 
 namespace mq {
@@ -111,44 +112,6 @@ __device__ __forceinline__ int sum_of_wave(int total) {
     return total;
 }
 
-// The `block`-th block of BM places, counted expert by expert: no block holds places of two experts.  `bound(e)`: where the places of
-// expert e begin, e = 0 .. E (data: whatever it holds, places stay below T).
-struct Block {
-    int expert, place, count;  // count = 0: there is no such block
-};
-template <typename Bound>
-__device__ __forceinline__ Block find_block(int T, int E, int block, int BM, Bound &&bound, int *blocks = nullptr) {
-    // a lane for each expert: blocks up to and with it by a prefix sum
-    const int lane = threadIdx.x & 63;
-    Block found{0, 0, 0};
-    int before = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        const int e = e0 + lane;
-        int lo = 0, hi = 0;
-        if (e < E) {
-            lo = min(max(bound(e), 0), T);
-            hi = min(max(bound(e + 1), lo), T);
-        }
-        const int mine = (int)(((uint32_t)(hi - lo) + (uint32_t)BM - 1u) / (uint32_t)BM);
-        int upto = before + mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o, 64) - before;
-            if (lane >= o) upto += v;
-        }
-        const uint64_t past = __ballot(upto > block);
-        if (past && found.count == 0) {
-            const int at = __builtin_ctzll(past), nth = block - __builtin_amdgcn_readlane(upto - mine, at);
-            const int place = __builtin_amdgcn_readlane(lo, at) + nth * BM;
-            // (bounds that descend may wrap the sums: nothing is found then)
-            if ((uint32_t)nth < (uint32_t)__builtin_amdgcn_readlane(mine, at)) found = Block{e0 + at, place, min(BM, __builtin_amdgcn_readlane(hi, at) - place)};
-            if (!blocks) return found;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-    if (blocks) *blocks = before;
-    return found;
-}
 __device__ __forceinline__ Block find_block(const Int8Args &a, int block, int BM) {
     if (!a.offsets) return Block{0, block * BM, min(BM, a.T - block * BM)};
     return find_block(a.T, a.E, block, BM, [&](int e) { return a.offsets[e]; });

@@ -61,38 +61,14 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
         int range;
     };
     const int splits = CUT ? ranges.splits : 1, stages = (a.K + 127) / 128;
-    // Four blocks of places at a time, all channels for them; products by expert: of one expert, whose codes are then read from memory once.
-    auto unit_at = [&](int lid) {
-        constexpr int GROUP = 4;
-        int first = 0, blocks = tiles_m;   // the expert's
-        Block b{0, 0, a.T};
-        if (a.offsets) {
-            b = find_block(a.T, a.E, lid / tiles_n, unit, bound);
-            const int lo = min(max(bound(b.expert), 0), a.T), hi = min(max(bound(b.expert + 1), lo), a.T);
-            if (b.count <= 0) return Tile{b, 0, 0};
-            first = lid / tiles_n - (b.place - lo) / unit;
-            blocks = (int)(((uint32_t)(hi - lo) + (uint32_t)unit - 1u) / (uint32_t)unit);
-            b.place = lo;
-            b.count = hi - lo;
-        }
-        const int local = lid - first * tiles_n, width = GROUP * tiles_n;
-        const int first_m = local / width * GROUP, gsz = min(blocks - first_m, GROUP);
-        const int down = (first_m + local % width % gsz) * unit;
-        return Tile{Block{b.expert, b.place + down, min(unit, b.count - down)}, local % width / gsz * unit, 0};
-    };
     // the first tile from id on, in steps of the grid, that is not empty (quarters may be): id is left at it, or past the last
     auto tile_from = [&](int &id) {
         Tile t = {};
         for (; id < total * splits; id += (int)gridDim.x) {
             const int at = (int)xcd_contiguous_id(id, total * splits), lid = CUT ? at % total : at;
-            t = unit_at(tiles.first + (QUARTERS ? lid / 4 : lid));
-            if (QUARTERS) {
-                const int down = (lid & 1) * T::TM;
-                t.b.place += down;
-                t.b.count = min(t.b.count - down, T::TM);
-                t.n0 += (lid >> 1 & 1) * T::TN;
-            }
-            if (CUT) t.range = at / total;
+            Unit u = unit_at<unit>(tiles.first + (QUARTERS ? lid / 4 : lid), a.T, a.E, a.offsets != nullptr, tiles_m, tiles_n, bound);
+            if (QUARTERS) u = quarter_of<unit>(u, lid & 3);
+            t = Tile{u.b, u.n0, CUT ? at / total : 0};
             if (t.b.count > 0 && t.n0 < a.N) break;
         }
         return t;
