@@ -214,7 +214,7 @@ __device__ __forceinline__ void int8_tiles(const Int8Args &a, const Int8Tiles &t
             for (int rb = 0; rb < RB; ++rb) {
                 float y[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = int8_output(acc[rb][tb][e], sum[tb], scale[tb], ka[rb][e], kb[rb][e], a.offset);
+                for (int e = 0; e < 4; ++e) y[e] = int8_output<R8>(acc[rb][tb][e], sum[tb], scale[tb], ka[rb][e], kb[rb][e], a.offset);
                 if constexpr (GATED)
                     o[rb][0] = pack_bf16x2(gated_value(y[0], y[1], a.gate), gated_value(y[2], y[3], a.gate));
                 else
