@@ -533,7 +533,8 @@ mq_status mq_linear_fwd_int8_quantized(const int8_t *Xq, const float *scale, con
  *
  * mq_experts_fwd_int8: for every place p of expert e
  *     Y[p] = the layer of mq_linear_fwd_int8 with codes[e], alpha[e], zero[e] on token rows[p]
- * with the same bits as that call.  Group sizes are read on the device; an expert without tokens costs nothing.
+ * with the same bits as that call.  Group sizes are read on the device; an expert without tokens costs nothing.  The M tokens (past 2 GiB of
+ * them the T places) are quantized all, whichever of them have an expert: what is in the others is read, and shows nowhere.
  *   X        [M, K] bf16            rows [T] int32, values 0 .. M-1, or NULL: place p is token p (T <= M)
  *   offsets  [E + 1] int32, ascending, offsets[E] <= T; rows of Y from offsets[E] on are not written.  (Values outside of that
  *            give undefined outputs, but nothing outside the arrays is read or written.)

@@ -1,6 +1,9 @@
-// The product in 8-bit integers for many tokens: tiles through LDS.  Bound by the matrix core and its power: 8192 x 28672 x 3584 with a gate 700 us
-// (2.40 POP/s; the core is busy 61 % of the cycles at 1.7 GHz), 2011 x 14336 x 4096 83 us (2.85 POP/s before the clock goes down).  A tile's
-// operands come through LDS once per wave that needs them: 64 x 128 per wave reads 24 KB for 128 products of 16 cycles.  What counted:
+// The product in 8-bit integers for many tokens: tiles through LDS.  Bound by the matrix core, at the clock that its power allows where the launch is long
+// enough for that to show, and by the ends of tiles: 8192 x 28672 x 3584 with a gate 762 us under the counters (2.21 POP/s; the core is busy 61 % of
+// the cycles at 1.71 GHz), 2011 x 14336 x 4096 96 us (2.45 POP/s; 54 % at 2.22 GHz, two rounds for 1.75 of tiles).  A tile's operands come through
+// LDS once per wave that needs them: 64 x 128 per wave and stage reads 24 KB for 64 products of 16 cycles, 768 of the 2048 clocks for eight waves;
+// products with just these reads beside them reach 3.39 POP/s, without 3.56.  A tile's first stage waits for the stores of the tile before too: they are
+// counted with the loads and were issued behind them.  What counted:
 // stages of 128 k, whose rows are whole lines of the L2 (64 k: 8 % slower); products without a pause, operands of the next half replaced behind
 // the last product that uses them; the next tile's first stages on their way, and nothing spilled, while outputs are formed; those through LDS to
 // stores of 128 bytes side by side.

@@ -623,8 +623,8 @@ static DwPlan dw_plan(int64_t M, int64_t N, int64_t K, int batch) { return remem
 // MFMAs), without any code conversion.  The four
 // waves form a 2 x 2 grid over the tile.  HB = 4, a 256 x 256 tile, 128 x 128 per wave: 64 accumulators of 16 x 16 (all 256
 // accumulator registers), 16 operand reads per 64 MFMAs - the square wave tile is what keeps the LDS traffic (32 KB read + 16 KB
-// written per 16 tokens and compute unit, 94 bytes per clock at the matrix-core rate) under the 128 bytes per clock the LDS
-// delivers.  HB = 2, a 128 x 128 tile, 64 x 64 per wave: 16 accumulators, 8 reads per 16 MFMAs, two workgroups to a compute
+// written per 16 tokens and compute unit, 94 bytes per clock at the matrix-core rate) under what the LDS gives beside products
+// (256 bytes per clock for conflict-free reads alone).  HB = 2, a 128 x 128 tile, 64 x 64 per wave: 16 accumulators, 8 reads per 16 MFMAs, two workgroups to a compute
 // unit.  Stages are one 32-token step deep; five of them fill the LDS (HB = 2: half of it).
 //
 // TURN: the contraction index (tokens) runs across the rows of both operands, as the caller left them, and the LDS turns them on the

@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void dx_finish_kernel(DxArgs a, int mb) {
 // ============================================================================================
 // The main loop of dX with other names: Y[m, n] = sum over k of X[m, k] * code[n, k], one bit-width.  With a single bit-width a
 // wave of the forward kernel (32 channels) reads one activation operand from LDS per product, 128 bytes per clock and compute
-// unit at the matrix-core rate, which is all the LDS delivers; 64 channels per wave halve that.  The order of every sum and the
+// unit at the matrix-core rate, half of what the LDS delivers to reads alone; 64 channels per wave halve that.  The order of every sum and the
 // arithmetic of the epilogue are those of fwd_kernel.
 struct FwdWideArgs {
     DxArgs d;  // As[0] = X [M, K], QT = Q [N, K]; d.N is the contraction length K, d.K the channels N
