@@ -23,8 +23,9 @@
  *     launch and nothing is enqueued when a call fails.  After a failure no
  *     output is defined.
  *   - Device pointers must be 16-byte aligned and all matrices are dense
- *     (row stride = row length) except W, which has `ldw`, and the X of
- *     mq_quantize_tokens, which has `ldx`.
+ *     (row stride = row length) except W, which has `ldw`, the X of
+ *     mq_quantize_tokens, which has `ldx`, and the scores of mq_experts_choose,
+ *     which have `ld` and are 4-byte aligned.
  *   - Reentrant: nothing is kept between calls that a result depends on.  Two
  *     calls may run concurrently, from one or several host threads, on different
  *     streams when their buffers (workspace included) do not overlap.
@@ -556,8 +557,80 @@ mq_status mq_experts_fwd_int8(const uint16_t *X, int64_t M, const int32_t *rows,
 mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place, const float *weight, int64_t T, int64_t M, int64_t top,
                              int64_t N, uint16_t *out, void *hip_stream);
 
+/*
+ * Planes with group scales: a row's K inputs are cut into groups of `group`, each with an alpha and a z of its own (the paper has one pair
+ * per output channel, section 3.1.1; groups are the usual refinement for 4 and 2 bits).  Nothing of its own makes them: the groups of a
+ * dense W [N, K] are the rows of W as [N * K / group, group], so mq_quantize_int8 on that view gives codes [N, K] and alpha, z
+ * [N, K / group], mq_slice packs the codes as [N, K] and mq_params_to_bf16 rounds N * K / group pairs.  (Codes c' of another r-bit
+ * quantizer, W = a' (c' - z'), are the plane of c' with alpha = a' / 2^(8-r) and z = 2^(8-r) z', both exact in bf16 if a', z' are.)
+ *
+ * mq_gemv_grouped, for up to 16 tokens:
+ *     y[b,n] = sum_g alpha[n,g] * (2^(8-r) sum_{k in g} code[n,k] x[b,k] - z[n,g] sum_{k in g} x[b,k])
+ * the sums inside a group exact products in fp32, nothing rounded to fewer bits before y.
+ *   x       [B, K] bf16, 1 <= B <= 16
+ *   packed  [N, K*r/8] as mq_slice with MQ_FLAG_PACKED writes it, r in {8, 4, 2}
+ *   alpha_bf16, zero_bf16  [N, K / group] bf16
+ *   y       [B, N] bf16 out; may not overlap an input
+ * group a multiple of 32 (r = 2: of 64; MQ_ERR_ALIGN) that divides K; K itself is one pair per row.  K <= 2^20, N <= 2^25 (MQ_ERR_SHAPE
+ * beyond).  N == 0 is a no-op.  A token that holds an infinity or a NaN has outputs that are no numbers, no other token's are touched.  A token's
+ * outputs are the same bits whatever the other tokens are.
+ */
+mq_status mq_gemv_grouped(const uint16_t *x, const uint8_t *packed, const uint16_t *alpha_bf16, const uint16_t *zero_bf16,
+                          int64_t B, int64_t N, int64_t K, int64_t group, int r, uint16_t *y, void *hip_stream);
+
+/*
+ * A router's choice: the `top` largest scores of every token, largest first, equal ones by the lowest index, and their weights
+ *     weight[m,j] = exp(scores[m, ids[m,j]]) / sum_e exp(scores[m,e])
+ * the sum over all E experts, or over the chosen ones with MQ_FLAG_RENORMALIZE (fp32 throughout).
+ *   scores  [M, ld] fp32, ld >= E, 4-byte aligned.  -inf: not to be had (padding, masked experts).  A NaN is taken for +inf, and a
+ *           token with either has weights of NaN: it is chosen first and shows in that token's output.
+ *   flags   0 or MQ_FLAG_RENORMALIZE
+ *   ids     [M, top] int32 out: what mq_experts_route and mq_experts_ffn take; -1 where fewer than `top` scores are above -inf
+ *   weight  [M, top] fp32 out; 0 where the id is -1
+ * 1 <= E <= 1024, 1 <= top <= min(E, 32), M <= 2^25.  M == 0 is a no-op.
+ *
+ * mq_experts_choose_bwd: the gradient of the weights back to the scores, the choice held:
+ *     all experts:          dscores[m,e] = p[m,e] * (sum_{j: ids[m,j] = e} dweight[m,j] - mean)        p = softmax(scores)
+ *     MQ_FLAG_RENORMALIZE:  dscores[m,e] = sum_{j: ids[m,j] = e} weight[m,j] * (dweight[m,j] - mean)   (scores are not read)
+ *     mean = sum_j weight[m,j] dweight[m,j]
+ *   ids, weight  as mq_experts_choose wrote them; an id outside 0 .. E-1 is no choice, its weight and dweight are not looked at
+ *   dweight      [M, top] fp32
+ *   dscores      [M, E] fp32 out (dense); may not overlap an input
+ */
+enum { MQ_FLAG_RENORMALIZE = 256 };
+mq_status mq_experts_choose(const float *scores, int64_t M, int64_t E, int64_t ld, int64_t top, uint32_t flags, int32_t *ids,
+                            float *weight, void *hip_stream);
+mq_status mq_experts_choose_bwd(const float *scores, int64_t ld, const int32_t *ids, const float *weight, const float *dweight,
+                                int64_t M, int64_t E, int64_t top, uint32_t flags, float *dscores, void *hip_stream);
+
+/*
+ * A whole feed-forward layer of experts for up to 16 tokens in two launches, on planes with group scales (mq_experts_route and
+ * mq_experts_fwd_int8 are the way for more):
+ *     y_b = sum_j weight[b,j] * W_down[e] (act(W_gate[e] x_b) * W_up[e] x_b)        e = ids[b,j]
+ * (+ x_b with MQ_FLAG_FFN_RESIDUAL).  Products as mq_gemv_grouped forms them; fp32 up to y, only the gated products are held in 16
+ * significant bits in between.  Each expert's planes are read once, those of experts that nobody chose not at all.
+ *   x        [B, d] bf16, 1 <= B <= 16
+ *   layer    HOST descriptor as for mq_ffn_mixnmatch, its arrays those of all experts, one after the other: gate_up [E, 2F, d*r/8] (row
+ *            2 f = gate row f, row 2 f + 1 = up row f), down [E, d, F*r/8], alpha_gu, zero_gu bf16 [E, 2F, d / group], alpha_dn, zero_dn
+ *            bf16 [E, d, F / group]; r in {8, 4, 2}
+ *   ids      [B, top] int32; an id outside 0 .. E-1 is no choice (its weight is not looked at); an id that a token has twice counts
+ *            with both weights
+ *   weight   [B, top] fp32
+ *   group    inputs of a group in both planes, limits as for mq_gemv_grouped; 0 = one pair per row (then d and F have to be multiples of 32,
+ *            r = 2: of 64)
+ *   flags    MQ_FLAG_FFN_SILU (GELU in its tanh form otherwise), MQ_FLAG_FFN_RESIDUAL
+ *   y        [B, d] bf16 out; may not overlap an input.  A token without a choice gets zeros (with the residual, x)
+ *   ws       workspace of at least mq_workspace_bytes(MQ_OP_EXPERTS_FFN, B * top, F, d, 1)
+ * 1 <= top <= 16, 1 <= E <= 1024, d, F <= 2^20.
+ */
+enum { MQ_OP_EXPERTS_FFN = 11 };
+mq_status mq_experts_ffn(const uint16_t *x, const mq_ffn_layer *layer, const int32_t *ids, const float *weight, int64_t B, int64_t top,
+                         int64_t E, int64_t d, int64_t F, int64_t group, uint32_t flags, uint16_t *y, void *ws, size_t ws_bytes,
+                         void *hip_stream);
+
 /* Bytes of workspace for `op` at these sizes (0 on invalid arguments).  MQ_OP_FFN_DECODE: M = B, N = F, K = d.
  * MQ_OP_GEMV: M = B, nr = r (bits per code).  MQ_OP_EXPERTS_ROUTE: M = choices (tokens times top), N = E, K is not looked at.
+ * MQ_OP_EXPERTS_FFN: M = choices (1 .. 256), N = F, K = d.
  *
  * MQ_OP_LINEAR_FWD, MQ_OP_LINEAR_FWD_L2, MQ_OP_LINEAR_BWD, MQ_OP_LINEAR_BWD_CLIP: the bytes do not always grow with M.
  * Where few tokens would leave most of the GPU idle, contractions are cut into ranges whose fp32 partial sums (at most

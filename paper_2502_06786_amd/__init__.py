@@ -12,6 +12,7 @@ _BINDING_NAMES = {
     "mq_matquant_l2_loss", "MQ_OP_L2_LOSS", "MQ_FLAG_LOSS_MIX", "mq_linear_fwd_multi_l2", "MQ_OP_LINEAR_FWD_L2", "mq_linear_bwd_clip", "MQ_OP_LINEAR_BWD_CLIP", "mq_affine_weight", "mq_affine_input", "mq_affine_bwd", "MQ_OP_AFFINE_BWD", "mq_gated_unit_fwd", "mq_gated_unit_bwd", "mq_linear_fwd_multi_noalloc", "mq_linear_bwd_gated", "mq_slice_multi", "mq_linear_fwd_multi_gated", "mq_gemv_sliced_ws", "MQ_OP_GEMV",
     "mq_quantize_tokens", "mq_linear_fwd_int8", "mq_linear_fwd_int8_quantized", "mq_experts_route", "mq_experts_fwd_int8", "mq_experts_combine",
     "MQ_OP_LINEAR_FWD_INT8", "MQ_OP_EXPERTS_ROUTE", "MQ_OP_EXPERTS_FWD_INT8", "MQ_FLAG_GATED", "MQ_FLAG_FFN_SILU",
+    "mq_gemv_grouped", "mq_experts_choose", "mq_experts_choose_bwd", "mq_experts_ffn", "MQ_OP_EXPERTS_FFN", "MQ_FLAG_RENORMALIZE",
 }
 
 

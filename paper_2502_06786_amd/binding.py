@@ -34,6 +34,8 @@ MQ_FLAG_LOSS_MIX = 64
 MQ_FLAG_FFN_SILU = 16
 MQ_FLAG_FFN_RESIDUAL = 32
 MQ_FLAG_GATED = 128
+MQ_FLAG_RENORMALIZE = 256
+MQ_OP_EXPERTS_FFN = 11
 
 EXPORTS = ["mq_quantize_int8", "mq_slice", "mq_linear_fwd_multi", "mq_linear_bwd", "mq_gemv_sliced",
            "mq_params_to_bf16", "mq_workspace_bytes", "mq_status_string",
@@ -41,7 +43,7 @@ EXPORTS = ["mq_quantize_int8", "mq_slice", "mq_linear_fwd_multi", "mq_linear_bwd
            "mq_affine_weight", "mq_affine_input", "mq_affine_bwd", "mq_gated_unit_fwd", "mq_gated_unit_bwd",
            "mq_linear_fwd_multi_noalloc", "mq_linear_bwd_gated", "mq_linear_fwd_multi_gated", "mq_slice_multi", "mq_gemv_sliced_ws",
            "mq_quantize_tokens", "mq_linear_fwd_int8", "mq_linear_fwd_int8_quantized", "mq_experts_route", "mq_experts_fwd_int8",
-           "mq_experts_combine"]
+           "mq_experts_combine", "mq_gemv_grouped", "mq_experts_choose", "mq_experts_choose_bwd", "mq_experts_ffn"]
 
 
 class MqError(RuntimeError):
@@ -108,6 +110,10 @@ def _load() -> ctypes.CDLL:
     lib.mq_experts_route.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.mq_experts_fwd_int8.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, u32, vp, vp, sz, vp]
     lib.mq_experts_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp]
+    lib.mq_gemv_grouped.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, ci, vp, vp]
+    lib.mq_experts_choose.argtypes = [vp, i64, i64, i64, i64, u32, vp, vp, vp]
+    lib.mq_experts_choose_bwd.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, u32, vp, vp]
+    lib.mq_experts_ffn.argtypes = [vp, ctypes.POINTER(_FfnLayer), vp, vp, i64, i64, i64, i64, i64, i64, u32, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("mq_workspace_bytes", "mq_status_string"):
             getattr(lib, name).restype = ci
@@ -714,3 +720,103 @@ def mq_experts_combine(Y, place, weight, out=None):
                                  _ptr(out, torch.bfloat16), _stream())
     _check(st, "mq_experts_combine")
     return out
+
+
+def _here(*tensors):
+    """The library launches on the current device's stream: tensors of another device are refused."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must live on the current GPU")
+
+
+def mq_gemv_grouped(x, packed, alpha_bf16, zero_bf16, r: int, K: int, group: int, y=None):
+    """x bf16 [B, K], packed uint8 [N, K*r/8], alpha and zero bf16 [N, K/group] -> y bf16 [B, N]."""
+    B = x.shape[0]
+    N = packed.shape[0]
+    if group < 1 or K % group != 0:
+        raise ValueError("group does not divide K")
+    if x.shape != (B, K) or packed.shape != (N, K * r // 8) or alpha_bf16.shape != (N, K // group) or zero_bf16.shape != alpha_bf16.shape:
+        raise ValueError("shape mismatch")
+    if y is None:
+        y = torch.empty(B, N, dtype=torch.bfloat16, device=x.device)
+    elif y.shape != (B, N):
+        raise ValueError("y has another shape")
+    _here(x, packed, alpha_bf16, zero_bf16, y)
+    st = _lib.mq_gemv_grouped(_ptr(x, torch.bfloat16), _ptr(packed, torch.uint8), _ptr(alpha_bf16, torch.bfloat16),
+                              _ptr(zero_bf16, torch.bfloat16), B, N, K, group, r, _ptr(y, torch.bfloat16), _stream())
+    _check(st, "mq_gemv_grouped")
+    return y
+
+
+def _scores(scores):
+    """(pointer, M, E, row stride) of a router's scores."""
+    if scores.dtype is not torch.float32 or not scores.is_cuda or scores.dim() != 2 or (scores.shape[1] > 1 and scores.stride(1) != 1):
+        raise ValueError("scores must be a 2-D fp32 GPU tensor with unit column stride")
+    M, E = scores.shape
+    return scores.data_ptr(), M, E, scores.stride(0) if M > 1 else max(E, scores.stride(0))
+
+
+def mq_experts_choose(scores, top: int, renormalize: bool = False, ids=None, weight=None):
+    """The `top` largest of a router's scores fp32 [M, E] (row stride allowed): (ids int32 [M, top], weight fp32 [M, top]), the weights
+    out of the softmax over all experts or, with renormalize, over the chosen ones."""
+    p, M, E, ld = _scores(scores)
+    ids = torch.empty(M, top, dtype=torch.int32, device=scores.device) if ids is None else ids
+    weight = torch.empty(M, top, dtype=torch.float32, device=scores.device) if weight is None else weight
+    if ids.shape != (M, top) or weight.shape != (M, top):
+        raise ValueError("outputs do not match scores and top")
+    _here(scores, ids, weight)
+    st = _lib.mq_experts_choose(p, M, E, ld, top, MQ_FLAG_RENORMALIZE if renormalize else 0, _ptr(ids, torch.int32),
+                                _ptr(weight, torch.float32), _stream())
+    _check(st, "mq_experts_choose")
+    return ids, weight
+
+
+def mq_experts_choose_bwd(scores, ids, weight, dweight, renormalize: bool = False, dscores=None):
+    """Gradient of the weights of mq_experts_choose back to its scores: dscores fp32 [M, E]."""
+    p, M, E, ld = _scores(scores)
+    top = ids.shape[1]
+    if ids.shape != (M, top) or weight.shape != ids.shape or dweight.shape != ids.shape:
+        raise ValueError("scores, ids, weight and dweight differ in shape")
+    dscores = torch.empty(M, E, dtype=torch.float32, device=scores.device) if dscores is None else dscores
+    if dscores.shape != (M, E):
+        raise ValueError("dscores has another shape")
+    _here(scores, ids, weight, dweight, dscores)
+    st = _lib.mq_experts_choose_bwd(p, ld, _ptr(ids, torch.int32), _ptr(weight, torch.float32), _ptr(dweight, torch.float32), M, E, top,
+                                    MQ_FLAG_RENORMALIZE if renormalize else 0, _ptr(dscores, torch.float32), _stream())
+    _check(st, "mq_experts_choose_bwd")
+    return dscores
+
+
+def mq_experts_ffn(x, layer, ids, weight, F: int, group: int = 0, silu: bool = False, residual: bool = False, y=None, ws=None):
+    """A feed-forward layer of experts for up to 16 tokens: x bf16 [B, d], ids int32 and weight fp32 [B, top] -> y bf16 [B, d].
+    layer: a dict with the device tensors gate_up uint8 [E, 2F, d*r/8], down uint8 [E, d, F*r/8], alpha_gu, zero_gu bf16
+    [E, 2F, d/group], alpha_dn, zero_dn bf16 [E, d, F/group] and the int r; group 0: one pair per row."""
+    B, d = x.shape
+    r = int(layer["r"])
+    gate_up, down, agu, zgu, adn, zdn = (layer[k] for k in ("gate_up", "down", "alpha_gu", "zero_gu", "alpha_dn", "zero_dn"))
+    E = gate_up.shape[0]
+    if group < 0 or (group and (d % group != 0 or F % group != 0)):
+        raise ValueError("group does not divide d and F")
+    gd, gF = (d // group, F // group) if group else (1, 1)
+    if gate_up.shape != (E, 2 * F, d * r // 8) or down.shape != (E, d, F * r // 8):
+        raise ValueError("plane shapes do not match d, F, r")
+    if agu.numel() != E * 2 * F * gd or zgu.numel() != agu.numel() or adn.numel() != E * d * gF or zdn.numel() != adn.numel():
+        raise ValueError("parameter sizes do not match d, F, group")
+    top = ids.shape[1]
+    if ids.shape != (B, top) or weight.shape != ids.shape:
+        raise ValueError("x, ids and weight differ in shape")
+    if y is None:
+        y = torch.empty(B, d, dtype=torch.bfloat16, device=x.device)
+    elif y.shape != (B, d):
+        raise ValueError("y has another shape")
+    if ws is None:
+        ws = torch.empty(max(mq_workspace_bytes(MQ_OP_EXPERTS_FFN, B * top, F, d, 1), 16), dtype=torch.uint8, device=x.device)
+    _here(x, gate_up, down, agu, zgu, adn, zdn, ids, weight, y, ws)
+    c_layer = _FfnLayer(_ptr(gate_up, torch.uint8), _ptr(down, torch.uint8), _ptr(agu, torch.bfloat16), _ptr(zgu, torch.bfloat16),
+                        _ptr(adn, torch.bfloat16), _ptr(zdn, torch.bfloat16), r)
+    flags = (MQ_FLAG_FFN_SILU if silu else 0) | (MQ_FLAG_FFN_RESIDUAL if residual else 0)
+    st = _lib.mq_experts_ffn(_ptr(x, torch.bfloat16), ctypes.byref(c_layer), _ptr(ids, torch.int32), _ptr(weight, torch.float32), B, top, E, d, F,
+                             group, flags, _ptr(y, torch.bfloat16), _ptr(ws, torch.uint8), ws.numel(), _stream())
+    _check(st, "mq_experts_ffn")
+    return y
