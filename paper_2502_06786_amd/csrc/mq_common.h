@@ -91,7 +91,7 @@ size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K, bool grouped);
 // workspace of mq_experts_route for n choices (mq_experts.hip)
 size_t route_workspace_bytes(int64_t n, int64_t E);
 // workspace of mq_experts_ffn for n choices (mq_experts_ffn.hip)
-size_t experts_ffn_workspace_bytes(int64_t n, int64_t F);
+size_t experts_ffn_workspace_bytes(int64_t n, int64_t F, int64_t d);
 // G[i] [N, K] = lambda_i dY_i^T X for nr gradients against one X (mq_linear.hip).  dw_each_bytes: the workspace it can use, or
 // the least that it works with.
 size_t dw_each_bytes(int64_t M, int64_t N, int64_t K, int nr, bool least = false);

@@ -6,15 +6,18 @@
 
 namespace mq {
 
-// y[t, n] = sum over groups of alpha (2^s sum code x - z sum x).  A wave takes 16 rows of the plane (the matrix core's columns: lane
-// & 15) and all 16 places for tokens (its rows).  A row is cut into chunks of C codes, each inside one group: the four quarters of the
-// wave (lane >> 4) take C / 4 consecutive codes of it each, from one load of C r / 32 bytes, so one 16x16x32 product takes 8 codes of
-// every quarter and never mixes groups.  Two products run side by side: tokens x codes and tokens x ones, whose result is sum x in the
-// very lanes that hold the tokens' products; both are whole sums in fp32 before they meet alpha and z.  Codes of 4 and 2 bits enter as
-// 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of them), which sum x takes out again.
+// y[t, n] = sum over groups of alpha (2^s sum code x - z sum x).  A wave takes tiles of 16 rows of the plane (the matrix core's columns: lane
+// & 15) and up to 16 tokens (its rows), 32 codes to a step.  Two products run side by side: tokens x codes and tokens x ones, whose result is
+// sum x in the very lanes that hold the tokens' products; both are whole sums in fp32 over a chunk (a part of one group) before they meet
+// alpha and z.  Codes of 4 and 2 bits enter as 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of
+// them), which sum x takes out again.
 //
-// In operand order a register holds codes j and j + 4 (r = 4; j and j + 8 for r = 2) of the quarter's run, since that is what one shift and
-// mask leaves.  Tokens in their own order are turned to it in registers; the layer's gated products are stored in it.
+// Memory is read in pieces of a row, its 128-byte lines, by eight neighbouring lanes (and tokens alike): lanes that lie apart cost the address unit a
+// cycle each, 64 for a load whose lanes are all in different rows.  A wave's own part of LDS turns pieces into the matrix core's operands; pieces under
+// way stand in registers, of which a compute unit has three times as much as LDS.
+//
+// In operand order a register holds codes j and j + 4 (r = 4; j and j + 8 for r = 2) of a lane's run of 8 (16), since that is what one shift and
+// mask leaves.
 constexpr int kGroupedTokens = 16, kGroupedRows = 16;
 
 template <int R>
@@ -30,75 +33,24 @@ __device__ __forceinline__ int operand_place(int k) {
 
 // group of a chunk, cpg chunks to a group
 struct GroupOf {
-    uint32_t cpg, magic;  // magic = ceil(2^32 / cpg): exact while chunk * cpg < 2^32
-    __device__ __forceinline__ uint32_t operator()(uint32_t chunk) const { return cpg == 1 ? chunk : __umulhi(chunk, magic); }
+    uint32_t magic, whole;  // ceil(2^32 / cpg), 0 (exact while chunk * cpg < 2^32); for cpg = 1: 0, all bits
+    __device__ __forceinline__ uint32_t operator()(uint32_t chunk) const { return __umulhi(chunk, magic) + (chunk & whole); }
 };
-inline GroupOf group_of(int64_t cpg) { return GroupOf{(uint32_t)cpg, cpg == 1 ? 0u : (uint32_t)(((1ull << 32) + cpg - 1) / cpg)}; }
+inline GroupOf group_of(int64_t cpg) {
+    return cpg == 1 ? GroupOf{0u, ~0u} : GroupOf{(uint32_t)(((1ull << 32) + cpg - 1) / cpg), 0u};
+}
 
-// codes of a chunk: the most that a load of 16 bytes to a lane takes, as far as groups allow it
-template <int R>
-constexpr int kChunkMost = 512 / R;
-template <int R>
-constexpr int kChunkLeast = R == 2 ? 64 : 32;
-// inputs of a group have to be a whole number of 16-byte pieces of codes and of matrix products
+// inputs of a group have to be whole steps of the matrix core and whole pieces of 16 bytes
 inline int64_t group_unit(int r) { return r == 2 ? 64 : 32; }
+// codes of a chunk: those of a piece, or as far as groups allow it
 inline int chunk_codes(int r, int64_t group) {
     int c = 512 / r;
     while (group % c != 0) c >>= 1;
     return c;
 }
 
-template <int N>
-struct Dwords;
-template <>
-struct Dwords<1> {
-    typedef uint32_t type;
-};
-template <>
-struct Dwords<2> {
-    typedef u32x2 type;
-};
-template <>
-struct Dwords<4> {
-    typedef u32x4 type;
-};
-
 __device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-
-// the eight codes of step s out of a lane's run of a chunk, as bf16
-template <int R>
-__device__ __forceinline__ u32x4 codes_operand(const uint32_t *w, int s) {
-    u32x4 o;
-    if constexpr (R == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = ((w[s] >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-    } else if constexpr (R == 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = ((w[s >> 1] >> (8 * (s & 1) + 2 * i)) & 0x00030003u) | 0x43004300u;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t d = w[2 * s + (i >> 1)];
-            const float lo = (float)((d >> (16 * (i & 1))) & 0xFFu), hi = (float)((d >> (16 * (i & 1) + 8)) & 0xFFu);
-            o[i] = halves_hi(__float_as_uint(lo), __float_as_uint(hi));  // (0 .. 255 are bf16 numbers)
-        }
-    }
-    return o;
-}
-
-// step s of a lane's run of tokens that are stored in their own order
-template <int R>
-__device__ __forceinline__ u32x4 token_operand(const u32x4 *x, int s) {
-    if constexpr (R == 4)
-        return u32x4{halves_lo(x[s].x, x[s].z), halves_hi(x[s].x, x[s].z), halves_lo(x[s].y, x[s].w), halves_hi(x[s].y, x[s].w)};
-    if constexpr (R == 2) {
-        const u32x4 a = x[s & ~1], b = x[s | 1];
-        if (s & 1) return u32x4{halves_lo(a.z, b.z), halves_hi(a.z, b.z), halves_lo(a.w, b.w), halves_hi(a.w, b.w)};
-        return u32x4{halves_lo(a.x, b.x), halves_hi(a.x, b.x), halves_lo(a.y, b.y), halves_hi(a.y, b.y)};
-    }
-    return x[s];
-}
 
 __device__ __forceinline__ f32x4 mfma_tokens(u32x4 tokens, u32x4 codes, f32x4 c) {
     Frag8 a, b;
@@ -107,69 +59,227 @@ __device__ __forceinline__ f32x4 mfma_tokens(u32x4 tokens, u32x4 codes, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
 }
 
-// One lane's row of the plane and one lane's token, both from the start of its quarter's run of chunk 0.
-struct GroupedLane {
-    const uint8_t *codes;
-    const uint16_t *alpha, *zero;  // of the row, group 0
-    const uint16_t *x;             // the token, or its leading bf16 part in operand order
-    const uint16_t *rest;          // what the leading part leaves (bf16, operand order), with PARTS == 2
+constexpr int kHalves = 2, kPieces = 2;  // 64-byte halves of a piece, pieces of a stretch
+template <int R>
+constexpr int kHalfCodes = 512 / R;
+template <int R>
+constexpr int kStretchCodes = kPieces * kHalves * kHalfCodes<R>;
+
+// T: tokens that are loaded, 4, 8 or 16 (the rows of the matrix core behind them repeat them); C codes to a chunk; RG tiles of 16 rows.
+template <int R, int C, int RG, int T>
+struct Grouped {
+    static constexpr int PC = kHalfCodes<R>, NC = PC / C, STEPS = C / 32;
+    static constexpr int XS = PC / 8;                                // 16-byte slots of a token in half a piece
+    static constexpr int XI = T * XS < 64 ? 1 : T * XS / 64;         // loads of them for a wave
+    static constexpr int CODES = RG * 2048, TOKENS = XI * 1024;      // bytes of LDS
+    static constexpr int LDS = CODES + TOKENS + RG * 4 * NC * 64;
 };
 
-// Adds SPAN codes from chunk `first` on (what is behind the last chunk is left out) to y: lane = row, component i = token 4 (lane >> 4) + i.
-// PARTS 1: tokens in their own order; 2: values as the sum of two bf16 numbers, both in operand order.
-template <int R, int C, int SPAN, int PARTS>
-__device__ __forceinline__ void grouped_span(const GroupedLane &p, int first, int chunks, GroupOf group, f32x4 &y) {
-    constexpr int NC = SPAN / C, STEPS = C / 32, DW = C * R / 128, NP = (NC + 3) / 4;
-    static_assert(NC >= 1 && SPAN % C == 0 && (R != 2 || STEPS % 2 == 0), "");
-    typedef typename Dwords<DW>::type Piece;
-    const int lane = threadIdx.x & 63, quarter = lane >> 4;
+// A stretch of a product that one wave does: two pieces of 16 RG rows.  Bases are the same for the whole wave.
+template <int XI>
+struct Stretch {
+    const uint8_t *codes;          // row 0 of the tiles, code 0 of the rows
+    const uint16_t *alpha, *zero;  // row 0 of the tiles, group 0
+    const uint16_t *x;
+    uint32_t token[XI];            // begin of the token that a lane loads for (values, from x)
+    int first;                     // first half piece
+    // the layer's down product: whose outputs a lane's y are
+    int count;                     // tokens
+    uint32_t tokens;               // those of components 0 .. 3, a byte each
+    f32x4 share;                   // their weights
+};
+// Which token a lane's i-th load of half a piece is for.
+template <typename G>
+__device__ __forceinline__ int load_token(int i) {
+    return (64 * i + (int)(threadIdx.x & 63)) / G::XS;
+}
+
+// Does stretch after stretch: next(s) gives the wave's next one or says that there is none, end(s, more) follows each (with more, next has
+// been asked for the one behind it already); products are added to y[tile] (lane & 15 = row, component i = token 4 (lane >> 4) + i).  While a piece is
+// multiplied the D - 1 behind it are on their way; nothing is requested behind the last stretch.  ORDERED: tokens are in operand order.  What lies behind the end of rows of K
+// inputs is read as their end again and counts for nothing.
+template <int R, int C, int RG, int T, bool ORDERED, int D, typename Next, typename End>
+__device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, int groups, GroupOf group, f32x4 (&y)[RG], Next next, End end) {
+    using G = Grouped<R, C, RG, T>;
+    constexpr int PC = G::PC, NC = G::NC, STEPS = G::STEPS, XS = G::XS, XI = G::XI;
+    static_assert((D == 1 || D == 2) && NC >= 1 && STEPS >= 1 && (R != 2 || STEPS % 2 == 0), "");
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // (places in LDS are computed here, for each stream anew, instead of being kept in registers around it)
+    const int li = lane & 15, quarter = lane >> 4, part = lane & 3;
+    const int bytes = K / 8 * R, chunks = K / C;
     const float step = (float)(1 << (8 - R));
-    union {
-        Piece piece[NC];
-        uint32_t dw[NC * DW];
-    } w;
-    uint32_t params[NP];
-    u32x4 x[PARTS][NC * STEPS];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = min(first + j, chunks - 1);
-        w.piece[j] = __builtin_nontemporal_load(reinterpret_cast<const Piece *>(p.codes + (int64_t)c * (C * R / 8)));
-    }
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {  // quarter q of the wave looks up chunk 4 i + q for all of them
-        const uint32_t g = group((uint32_t)min(first + 4 * i + quarter, chunks - 1));
-        params[i] = (uint32_t)p.alpha[g] | (uint32_t)p.zero[g] << 16;
-    }
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int64_t at = (int64_t)min(first + j, chunks - 1) * C;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            x[0][j * STEPS + s] = *reinterpret_cast<const u32x4 *>(p.x + at + 8 * s);
-            if constexpr (PARTS == 2) x[PARTS - 1][j * STEPS + s] = *reinterpret_cast<const u32x4 *>(p.rest + at + 8 * s);
-        }
-    }
     const u32x4 ones{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    uint32_t mask = R == 4 ? 0x000F000Fu : 0x00030003u, base = 0x43004300u;  // (in registers: one instruction for "and" and "or", which takes no two literals)
+    asm volatile("" : "+s"(mask), "+v"(base));
+    uint8_t *const lds_x = lds + G::CODES;
+    uint32_t *const lds_params = reinterpret_cast<uint32_t *>(lds_x + G::TOKENS);
+
+    uint32_t row_codes[RG][2], row_params[RG];
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        f32x4 dot{0.f, 0.f, 0.f, 0.f}, sum{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < RG; ++t) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const u32x4 codes = codes_operand<R>(w.dw + j * DW, s);
-            const u32x4 t = PARTS == 2 ? x[0][j * STEPS + s] : token_operand<R>(x[0] + j * STEPS, s);
-            dot = mfma_tokens(t, codes, dot);
-            sum = mfma_tokens(t, ones, sum);
-            if constexpr (PARTS == 2) {
-                dot = mfma_tokens(x[PARTS - 1][j * STEPS + s], codes, dot);
-                sum = mfma_tokens(x[PARTS - 1][j * STEPS + s], ones, sum);
+        for (int i = 0; i < 2; ++i) row_codes[t][i] = (uint32_t)min(16 * t + 8 * i + (lane >> 3), rows - 1) * (uint32_t)bytes;
+        row_params[t] = (uint32_t)min(16 * t + (lane >> 2), rows - 1) * (uint32_t)groups;
+    }
+    // 16-byte slots are spread over the banks by the row's, the token's number
+    const int codes_to = (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4);
+    const int codes_from = li * 128, codes_turn = li & 7;
+    int x_to[XI];
+#pragma unroll
+    for (int i = 0; i < XI; ++i) {
+        const int token = load_token<G>(i), slot = (64 * i + lane) % XS;
+        x_to[i] = token * (XS * 16) + ((slot ^ (token & (XS - 1) & 15)) << 4);
+    }
+    const int x_token = li % T, x_from = x_token * (XS * 16), x_turn = x_token & (XS - 1) & 15;
+
+    u32x4 w[D][RG][2], x[D][kHalves][XI];
+    uint16_t alpha[RG][NC], zero[RG][NC];
+    auto fetch = [&](const Stretch<XI> &s, int j, int slot) {
+        const uint32_t at = (uint32_t)min((s.first + kHalves * j) * 64 + (lane & 7) * 16, bytes - 16);
+#pragma unroll
+        for (int t = 0; t < RG; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[slot][t][i] = *reinterpret_cast<const u32x4 *>(s.codes + (row_codes[t][i] + at));
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < XI; ++i) {
+                const uint32_t v = s.token[i] + (uint32_t)min((s.first + kHalves * j + h) * PC + (64 * i + lane) % XS * 8, K - 8);
+                x[slot][h][i] = *reinterpret_cast<const u32x4 *>(s.x + v);
+            }
+    };
+    auto fetch_params = [&](const Stretch<XI> &s) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const uint32_t g = group((uint32_t)min(s.first * NC + 4 * i + part, chunks - 1));
+#pragma unroll
+            for (int t = 0; t < RG; ++t) {
+                alpha[t][i] = s.alpha[row_params[t] + g];
+                zero[t][i] = s.zero[row_params[t] + g];
             }
         }
-        const uint32_t az = (uint32_t)__builtin_amdgcn_ds_bpermute(((lane & 15) + 16 * (j & 3)) << 2, (int)params[j >> 2]);
-        const float alpha = first + j < chunks ? bf16_lo(az) : 0.f;  // (behind the last chunk: the last again, which counts for nothing)
-        const float scale = alpha * step, shift = alpha * __builtin_fmaf(step, kCodeOffset<R>, bf16_hi(az));
+    };
+    auto multiply = [&](const Stretch<XI> &s, int half, int slot) {
+        const int h = half % kHalves;
+        if (h == 0)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(scale, dot[i], __builtin_fmaf(-shift, sum[i], y[i]));
+            for (int t = 0; t < RG; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4 *>(lds + t * 2048 + i * 1024 + codes_to) = w[slot][t][i];
+#pragma unroll
+        for (int i = 0; i < XI; ++i) {
+            u32x4 v = x[slot][h][i];
+            if constexpr (!ORDERED && R == 4) v = u32x4{halves_lo(v.x, v.z), halves_hi(v.x, v.z), halves_lo(v.y, v.w), halves_hi(v.y, v.w)};
+            *reinterpret_cast<u32x4 *>(lds_x + x_to[i]) = v;
+        }
+        auto slot_of_x = [&](int at) { return *reinterpret_cast<const u32x4 *>(lds_x + x_from + ((at ^ x_turn) << 4)); };
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            f32x4 dot[RG], sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < RG; ++t) dot[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            uint32_t both[RG];
+#pragma unroll
+            for (int k0 = 0; k0 < STEPS; ++k0) {
+                const int k = c * STEPS + k0;
+                u32x4 v;
+                if constexpr (R != 2) {
+                    v = slot_of_x(4 * k + quarter);
+                } else if constexpr (ORDERED) {
+                    v = slot_of_x(8 * (k >> 1) + 2 * quarter + (k & 1));
+                } else {
+                    const u32x4 a = slot_of_x(8 * (k >> 1) + 2 * quarter), b = slot_of_x(8 * (k >> 1) + 2 * quarter + 1);
+                    v = k & 1 ? u32x4{halves_lo(a.z, b.z), halves_hi(a.z, b.z), halves_lo(a.w, b.w), halves_hi(a.w, b.w)}
+                              : u32x4{halves_lo(a.x, b.x), halves_hi(a.x, b.x), halves_lo(a.y, b.y), halves_hi(a.y, b.y)};
+                }
+                sum = mfma_tokens(v, ones, sum);
+#pragma unroll
+                for (int t = 0; t < RG; ++t) {
+                    const uint8_t *tile = lds + t * 2048 + codes_from;
+                    u32x4 o;
+                    if constexpr (R == 4) {
+                        const uint32_t d = *reinterpret_cast<const uint32_t *>(tile + (((4 * h + k) ^ codes_turn) << 4) + 4 * quarter);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] = ((d >> (4 * i)) & mask) | base;
+                    } else if constexpr (R == 2) {
+                        if (!(k & 1)) both[t] = *reinterpret_cast<const uint32_t *>(tile + (((4 * h + (k >> 1)) ^ codes_turn) << 4) + 4 * quarter);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] = ((both[t] >> (8 * (k & 1) + 2 * i)) & mask) | base;
+                    } else {
+                        const u32x2 d = *reinterpret_cast<const u32x2 *>(tile + (((4 * h + 2 * k + (quarter >> 1)) ^ codes_turn) << 4) + 8 * (quarter & 1));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {  // (0 .. 255 are bf16 numbers)
+                            const float lo = (float)((d[i >> 1] >> (16 * (i & 1))) & 0xFFu), hi = (float)((d[i >> 1] >> (16 * (i & 1) + 8)) & 0xFFu);
+                            o[i] = halves_hi(__float_as_uint(lo), __float_as_uint(hi));
+                        }
+                    }
+                    dot[t] = mfma_tokens(v, o, dot[t]);
+                }
+            }
+            const int chunk = half * NC + c;
+#pragma unroll
+            for (int t = 0; t < RG; ++t) {
+                const uint32_t az = lds_params[(t * 4 * NC + chunk) * 16 + li];
+                const float a = s.first * NC + chunk < chunks ? bf16_lo(az) : 0.f;
+                const float scale = a * step, shift = a * __builtin_fmaf(step, kCodeOffset<R>, bf16_hi(az));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[t][i] = __builtin_fmaf(scale, dot[t][i], __builtin_fmaf(-shift, sum[i], y[t][i]));
+                asm volatile("" : "+v"(y[t]));  // (done here: put off to where y is used, every chunk's sums would stay in registers)
+            }
+        }
+    };
+    Stretch<XI> s, n;
+    if (!next(s)) return;
+    fetch_params(s);
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // (in order, as in the loop: a wait counts the requests behind the one it is for)
+        fetch(s, j, j);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    auto body = [&](auto with_next) {
+#pragma unroll
+        for (int t = 0; t < RG; ++t)
+#pragma unroll
+            for (int i = 0; i < NC; ++i) lds_params[(t * 4 * NC + 4 * i + part) * 16 + (lane >> 2)] = (uint32_t)alpha[t][i] | (uint32_t)zero[t][i] << 16;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                multiply(s, kHalves * j + h, j % D);
+                __builtin_amdgcn_sched_barrier(0);  // (keeps the requests of later pieces and what unpacks them out of this one's registers)
+            }
+            if (j + D < kPieces) {
+                fetch(s, j + D, j % D);
+            } else if constexpr (decltype(with_next)::value) {
+                if (j + D == kPieces) fetch_params(n);
+                fetch(n, j + D - kPieces, j % D);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    while (next(n)) {
+        body(std::true_type{});
+        end(s, true);
+        s = n;
+    }
+    body(std::false_type{});
+    end(s, false);
+}
+
+// Adds up the tiles of the workgroup's waves (part: one place for each wave and tile) into those of the first one.
+template <int RG>
+__device__ __forceinline__ void join_waves(f32x4 *part, int wave, int waves, f32x4 (&y)[RG]) {
+    if (waves == 1) return;
+    const int lane = threadIdx.x & 63;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RG; ++t) part[(wave * RG + t) * 64 + lane] = y[t];
+    __syncthreads();
+    if (wave != 0) return;
+    for (int k = 1; k < waves; ++k)
+#pragma unroll
+        for (int t = 0; t < RG; ++t) y[t] += part[(k * RG + t) * 64 + lane];
 }
 
 // What is refused about a plane of `rows` rows and K inputs before a launch.

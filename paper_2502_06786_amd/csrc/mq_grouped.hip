@@ -1,4 +1,6 @@
 // Matrix-vector products with planes that have a scale and a zero-point for every group of inputs.
+#include <algorithm>
+
 #include "mq_grouped.h"
 
 namespace mq {
@@ -8,44 +10,49 @@ struct GroupedGemvArgs {
     const uint8_t *packed;  // [N, K R / 8]
     const uint16_t *alpha, *zero;  // [N, groups] bf16
     uint16_t *y;            // [B, N] bf16
-    int B, N, K, groups, chunks, ks;
+    int B, N, K, groups, ks;
     GroupOf group;
 };
 
-constexpr int kGroupedWaves = 16;
-// codes of a row that a wave has under way at a time, as far as its registers go
-constexpr int grouped_gemv_span(int c) { return c == 32 ? 256 : 512; }
+// waves of a workgroup at most: 16 leave 128 registers to each
+constexpr int gemv_waves(int R, int RG, int T, int D) { return R == 2 && (T == 16 || RG * D == 4) ? 8 : 16; }
 
-// A workgroup takes 16 rows (or a few times 16 where rows are short), its waves spans of 512 codes (256 where groups are short) of them in turn: all loads of a span
-// leave together, and what hides their latency is the other waves of the compute unit.  The waves' sums meet in LDS.
-template <int R, int C>
-__global__ __launch_bounds__(64 * kGroupedWaves) void gemv_grouped_kernel(GroupedGemvArgs a) {
-    constexpr int SPAN = grouped_gemv_span(C);
-    __shared__ f32x4 part[kGroupedWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, quarter = lane >> 4;
-    const int tile = wave / a.ks, ks = wave - tile * a.ks, tiles = (int)(blockDim.x >> 6) / a.ks;
-    const int row0 = ((int)blockIdx.x * tiles + tile) * kGroupedRows;
-    const int row = min(row0 + li, a.N - 1), token = min(li, a.B - 1);
-    GroupedLane p;
-    p.codes = a.packed + (int64_t)row * (a.K / 8 * R) + quarter * (C * R / 32);
-    p.alpha = a.alpha + (int64_t)row * a.groups;
-    p.zero = a.zero + (int64_t)row * a.groups;
-    p.x = a.x + (int64_t)token * a.K + quarter * (C / 4);
-    p.rest = nullptr;
-    f32x4 y{0.f, 0.f, 0.f, 0.f};
-    if (row0 < a.N)
-        for (int c = ks * (SPAN / C); c < a.chunks; c += a.ks * (SPAN / C))
-            grouped_span<R, C, SPAN, 1>(p, c, a.chunks, a.group, y);
-    if (a.ks > 1) {
-        part[wave][lane] = y;
-        __syncthreads();
-        if (ks != 0) return;
-        for (int k = 1; k < a.ks; ++k) y += part[wave + k][lane];
-    }
-    if (row0 + li >= a.N) return;
+// A workgroup takes 16 RG rows, its waves stretches of them in turn; the waves' sums meet in LDS.
+template <int R, int C, int RG, int T, int D>
+__global__ __launch_bounds__(64 * gemv_waves(R, RG, T, D)) void gemv_grouped_kernel(GroupedGemvArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    using G = Grouped<R, C, RG, T>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
+    const int row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.K + kStretchCodes<R> - 1) / kStretchCodes<R>;
+    f32x4 y[RG];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (4 * quarter + i < a.B) a.y[(int64_t)(4 * quarter + i) * a.N + row0 + li] = (uint16_t)float_to_bf16_bits(y[i]);
+    for (int t = 0; t < RG; ++t) y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int at = wave;
+    grouped_stream<R, C, RG, T, false, D>(
+        lds + wave * G::LDS, a.N - row0, a.K, a.groups, a.group, y,
+        [&](Stretch<G::XI> &s) {
+            if (at >= stretches) return false;
+            s.codes = a.packed + (int64_t)row0 * (a.K / 8 * R);
+            s.alpha = a.alpha + (int64_t)row0 * a.groups;
+            s.zero = a.zero + (int64_t)row0 * a.groups;
+            s.x = a.x;
+#pragma unroll
+            for (int i = 0; i < G::XI; ++i) s.token[i] = (uint32_t)(min(load_token<G>(i), a.B - 1) * a.K);
+            s.first = at * kPieces * kHalves;
+            at += a.ks;
+            return true;
+        },
+        [](const Stretch<G::XI> &, bool) {});
+    join_waves<RG>(reinterpret_cast<f32x4 *>(lds), wave, a.ks, y);
+    if (wave != 0) return;
+#pragma unroll
+    for (int t = 0; t < RG; ++t) {
+        const int row = row0 + 16 * t + li;
+        if (row >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (4 * quarter + i < a.B) a.y[(int64_t)(4 * quarter + i) * a.N + row] = (uint16_t)float_to_bf16_bits(y[t][i]);
+    }
 }
 
 mq_status grouped_check(const uint8_t *packed, const uint16_t *alpha, const uint16_t *zero, int64_t rows, int64_t K, int64_t group, int r) {
@@ -58,13 +65,34 @@ mq_status grouped_check(const uint8_t *packed, const uint16_t *alpha, const uint
     return MQ_OK;
 }
 
-template <int R, int C>
-static mq_status launch_gemv_grouped(GroupedGemvArgs a, hipStream_t st) {
-    const int spans = (int)cdiv(a.K, grouped_gemv_span(C)), turns = (int)cdiv(spans, kGroupedWaves);
-    a.ks = (int)cdiv(spans, turns);
-    const int tiles = a.ks >= 4 ? 1 : 4 / a.ks;
-    gemv_grouped_kernel<R, C><<<dim3((unsigned)cdiv(a.N, kGroupedRows * tiles)), dim3(64 * a.ks * tiles), 0, st>>>(a);
+template <int R, int C, int RG, int T, int D>
+static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
+    using G = Grouped<R, C, RG, T>;
+    const int64_t stretches = cdiv(a.K, kStretchCodes<R>), blocks = cdiv(a.N, kGroupedRows * RG);
+    // Waves of a workgroup: 12 on each compute unit where there is no more than a workgroup or two for each (4096 x 14336, B = 16: 11.8 us, with
+    // 14 waves instead of 10 12.9), otherwise 24, of which 16 to 20 are there at a time (73728 x 4608, B = 1: 34.9 us, half as many 39.4).
+    const int64_t wanted = cdiv(blocks <= 512 ? 3072 : 6144, blocks);
+    a.ks = (int)std::min<int64_t>({stretches, gemv_waves(R, RG, T, D), 163840 / G::LDS, wanted});
+    a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
+    const int lds = a.ks * G::LDS;
+    constexpr auto kernel = gemv_grouped_kernel<R, C, RG, T, D>;
+    if (lds > 65536 && !allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
+    kernel<<<dim3((unsigned)blocks), dim3(64 * a.ks), lds, st>>>(a);
     return launch_status();
+}
+
+// Tiles of a wave and pieces under way.  Two tiles share the tokens' way through LDS, which counts for 16 tokens from 8192 rows on (14336 x
+// 4096, B = 16: 10.2 us with two, 12.3 with one; 4096 x 14336: 14.4 and 11.8), for up to 4 where memory is kept busy by half as many
+// waves (73728 x 4608, B = 1, r = 4: 34.9 and 37.0 us; 28672 x 4096: 13.5 and 13.0), at two bits, which are bound by the vector unit, earlier
+// (28672 x 4096: 12.9 and 13.5).  Groups of 32 at four bits leave no registers for it (73728 x 4608: 57 and 51 us).
+template <int R, int C>
+static mq_status launch_gemv_grouped(const GroupedGemvArgs &a, hipStream_t st) {
+    if (a.B > 4) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 16, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 16, 1>(a, st);
+    if constexpr (R == 4 && C == 32) return launch_gemv_grouped_as<R, C, 1, 4, 2>(a, st);
+    if constexpr (R != 4 || C != 32) {
+        if (a.N >= (R == 4 ? 65536 : 16384)) return launch_gemv_grouped_as<R, C, 2, 4, 2>(a, st);
+        return launch_gemv_grouped_as<R, C, 1, 4, R == 2 ? 1 : 2>(a, st);
+    }
 }
 
 }  // namespace mq
@@ -78,7 +106,7 @@ extern "C" mq_status mq_gemv_grouped(const uint16_t *x, const uint8_t *packed, c
     if (!x || !y) return MQ_ERR_NULL;
     if (!aligned16(x) || !aligned16(y)) return MQ_ERR_ALIGN;
     const int c = chunk_codes(r, group);
-    const GroupedGemvArgs a{x, packed, alpha_bf16, zero_bf16, y, (int)B, (int)N, (int)K, (int)(K / group), (int)(K / c), 1, group_of(group / c)};
+    const GroupedGemvArgs a{x, packed, alpha_bf16, zero_bf16, y, (int)B, (int)N, (int)K, (int)(K / group), 1, group_of(group / c)};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
 #define MQ_GROUPED_CASE(R_, C_) \
     if (r == R_ && c == C_) return launch_gemv_grouped<R_, C_>(a, st);

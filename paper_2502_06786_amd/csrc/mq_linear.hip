@@ -1066,7 +1066,7 @@ extern "C" size_t mq_workspace_bytes(int op, int64_t M, int64_t N, int64_t K, in
     if (op == MQ_OP_GEMV)  // M = B, nr = bits per code
         return M < 1 || M > 16 || N < 0 || K < 1 || nr < 1 || nr > 8 ? 0 : std::max<size_t>(256, gemv_split_workspace_bytes(M, N, K, nr));
     if (op == MQ_OP_EXPERTS_ROUTE) return route_workspace_bytes(M, N);
-    if (op == MQ_OP_EXPERTS_FFN) return experts_ffn_workspace_bytes(M, N);
+    if (op == MQ_OP_EXPERTS_FFN) return experts_ffn_workspace_bytes(M, N, K);
     if (M < 0 || N < 0 || K < 0 || nr < 1 || nr > 3) return 0;
     if (op == MQ_OP_LINEAR_FWD || op == MQ_OP_LINEAR_FWD_L2)
         return fwd_layout(M, N, fwd_split_plan(M, N, K, nr), op == MQ_OP_LINEAR_FWD_L2).total;
