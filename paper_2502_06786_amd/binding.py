@@ -722,69 +722,75 @@ def mq_experts_combine(Y, place, weight, out=None):
     return out
 
 
-def _here(*tensors):
-    """The library launches on the current device's stream: tensors of another device are refused."""
-    dev = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError("tensors must live on the current GPU")
+def _dense(t, dtype, device: int) -> int:
+    """Pointer of a dense tensor of this type on the current device, on whose stream the library launches."""
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor on the current GPU, got {t.dtype} on {t.device}")
+    return t.data_ptr()
 
 
 def mq_gemv_grouped(x, packed, alpha_bf16, zero_bf16, r: int, K: int, group: int, y=None):
     """x bf16 [B, K], packed uint8 [N, K*r/8], alpha and zero bf16 [N, K/group] -> y bf16 [B, N]."""
-    B = x.shape[0]
-    N = packed.shape[0]
-    if group < 1 or K % group != 0:
-        raise ValueError("group does not divide K")
-    if x.shape != (B, K) or packed.shape != (N, K * r // 8) or alpha_bf16.shape != (N, K // group) or zero_bf16.shape != alpha_bf16.shape:
+    B, k = x.shape
+    N, row = packed.shape
+    if k != K or group < 1 or K % group != 0 or row * 8 != K * r or alpha_bf16.shape != (N, K // group) or zero_bf16.shape != (N, K // group):
         raise ValueError("shape mismatch")
     if y is None:
         y = torch.empty(B, N, dtype=torch.bfloat16, device=x.device)
     elif y.shape != (B, N):
         raise ValueError("y has another shape")
-    _here(x, packed, alpha_bf16, zero_bf16, y)
-    st = _lib.mq_gemv_grouped(_ptr(x, torch.bfloat16), _ptr(packed, torch.uint8), _ptr(alpha_bf16, torch.bfloat16),
-                              _ptr(zero_bf16, torch.bfloat16), B, N, K, group, r, _ptr(y, torch.bfloat16), _stream())
-    _check(st, "mq_gemv_grouped")
+    dev = torch._C._cuda_getDevice()
+    bf16 = torch.bfloat16
+    st = _lib.mq_gemv_grouped(_dense(x, bf16, dev), _dense(packed, torch.uint8, dev), _dense(alpha_bf16, bf16, dev), _dense(zero_bf16, bf16, dev),
+                              B, N, K, group, r, _dense(y, bf16, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if st:
+        _check(st, "mq_gemv_grouped")
     return y
 
 
-def _scores(scores):
+def _scores(scores, device: int):
     """(pointer, M, E, row stride) of a router's scores."""
-    if scores.dtype is not torch.float32 or not scores.is_cuda or scores.dim() != 2 or (scores.shape[1] > 1 and scores.stride(1) != 1):
-        raise ValueError("scores must be a 2-D fp32 GPU tensor with unit column stride")
     M, E = scores.shape
-    return scores.data_ptr(), M, E, scores.stride(0) if M > 1 else max(E, scores.stride(0))
+    step, unit = scores.stride()
+    if scores.dtype is not torch.float32 or scores.get_device() != device or (unit != 1 and E > 1):
+        raise ValueError("scores must be a 2-D fp32 tensor with unit column stride on the current GPU")
+    return scores.data_ptr(), M, E, step if M > 1 else max(E, step)
 
 
 def mq_experts_choose(scores, top: int, renormalize: bool = False, ids=None, weight=None):
     """The `top` largest of a router's scores fp32 [M, E] (row stride allowed): (ids int32 [M, top], weight fp32 [M, top]), the weights
     out of the softmax over all experts or, with renormalize, over the chosen ones."""
-    p, M, E, ld = _scores(scores)
-    ids = torch.empty(M, top, dtype=torch.int32, device=scores.device) if ids is None else ids
-    weight = torch.empty(M, top, dtype=torch.float32, device=scores.device) if weight is None else weight
+    dev = torch._C._cuda_getDevice()
+    p, M, E, ld = _scores(scores, dev)
+    if ids is None:
+        ids = torch.empty(M, top, dtype=torch.int32, device=scores.device)
+    if weight is None:
+        weight = torch.empty(M, top, dtype=torch.float32, device=scores.device)
     if ids.shape != (M, top) or weight.shape != (M, top):
         raise ValueError("outputs do not match scores and top")
-    _here(scores, ids, weight)
-    st = _lib.mq_experts_choose(p, M, E, ld, top, MQ_FLAG_RENORMALIZE if renormalize else 0, _ptr(ids, torch.int32),
-                                _ptr(weight, torch.float32), _stream())
-    _check(st, "mq_experts_choose")
+    st = _lib.mq_experts_choose(p, M, E, ld, top, MQ_FLAG_RENORMALIZE if renormalize else 0, _dense(ids, torch.int32, dev),
+                                _dense(weight, torch.float32, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if st:
+        _check(st, "mq_experts_choose")
     return ids, weight
 
 
 def mq_experts_choose_bwd(scores, ids, weight, dweight, renormalize: bool = False, dscores=None):
     """Gradient of the weights of mq_experts_choose back to its scores: dscores fp32 [M, E]."""
-    p, M, E, ld = _scores(scores)
-    top = ids.shape[1]
-    if ids.shape != (M, top) or weight.shape != ids.shape or dweight.shape != ids.shape:
+    dev = torch._C._cuda_getDevice()
+    p, M, E, ld = _scores(scores, dev)
+    shape = ids.shape
+    if len(shape) != 2 or shape[0] != M or weight.shape != shape or dweight.shape != shape:
         raise ValueError("scores, ids, weight and dweight differ in shape")
-    dscores = torch.empty(M, E, dtype=torch.float32, device=scores.device) if dscores is None else dscores
-    if dscores.shape != (M, E):
+    if dscores is None:
+        dscores = torch.empty(M, E, dtype=torch.float32, device=scores.device)
+    elif dscores.shape != (M, E):
         raise ValueError("dscores has another shape")
-    _here(scores, ids, weight, dweight, dscores)
-    st = _lib.mq_experts_choose_bwd(p, ld, _ptr(ids, torch.int32), _ptr(weight, torch.float32), _ptr(dweight, torch.float32), M, E, top,
-                                    MQ_FLAG_RENORMALIZE if renormalize else 0, _ptr(dscores, torch.float32), _stream())
-    _check(st, "mq_experts_choose_bwd")
+    f32 = torch.float32
+    st = _lib.mq_experts_choose_bwd(p, ld, _dense(ids, torch.int32, dev), _dense(weight, f32, dev), _dense(dweight, f32, dev), M, E, shape[1],
+                                    MQ_FLAG_RENORMALIZE if renormalize else 0, _dense(dscores, f32, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if st:
+        _check(st, "mq_experts_choose_bwd")
     return dscores
 
 
@@ -794,17 +800,18 @@ def mq_experts_ffn(x, layer, ids, weight, F: int, group: int = 0, silu: bool = F
     [E, 2F, d/group], alpha_dn, zero_dn bf16 [E, d, F/group] and the int r; group 0: one pair per row."""
     B, d = x.shape
     r = int(layer["r"])
-    gate_up, down, agu, zgu, adn, zdn = (layer[k] for k in ("gate_up", "down", "alpha_gu", "zero_gu", "alpha_dn", "zero_dn"))
+    gate_up, down = layer["gate_up"], layer["down"]
+    agu, zgu, adn, zdn = layer["alpha_gu"], layer["zero_gu"], layer["alpha_dn"], layer["zero_dn"]
     E = gate_up.shape[0]
     if group < 0 or (group and (d % group != 0 or F % group != 0)):
         raise ValueError("group does not divide d and F")
-    gd, gF = (d // group, F // group) if group else (1, 1)
+    gu, dn = (E * 2 * F * (d // group), E * d * (F // group)) if group else (E * 2 * F, E * d)
     if gate_up.shape != (E, 2 * F, d * r // 8) or down.shape != (E, d, F * r // 8):
         raise ValueError("plane shapes do not match d, F, r")
-    if agu.numel() != E * 2 * F * gd or zgu.numel() != agu.numel() or adn.numel() != E * d * gF or zdn.numel() != adn.numel():
+    if agu.numel() != gu or zgu.numel() != gu or adn.numel() != dn or zdn.numel() != dn:
         raise ValueError("parameter sizes do not match d, F, group")
     top = ids.shape[1]
-    if ids.shape != (B, top) or weight.shape != ids.shape:
+    if ids.shape != (B, top) or weight.shape != (B, top):
         raise ValueError("x, ids and weight differ in shape")
     if y is None:
         y = torch.empty(B, d, dtype=torch.bfloat16, device=x.device)
@@ -812,11 +819,13 @@ def mq_experts_ffn(x, layer, ids, weight, F: int, group: int = 0, silu: bool = F
         raise ValueError("y has another shape")
     if ws is None:
         ws = torch.empty(max(mq_workspace_bytes(MQ_OP_EXPERTS_FFN, B * top, F, d, 1), 16), dtype=torch.uint8, device=x.device)
-    _here(x, gate_up, down, agu, zgu, adn, zdn, ids, weight, y, ws)
-    c_layer = _FfnLayer(_ptr(gate_up, torch.uint8), _ptr(down, torch.uint8), _ptr(agu, torch.bfloat16), _ptr(zgu, torch.bfloat16),
-                        _ptr(adn, torch.bfloat16), _ptr(zdn, torch.bfloat16), r)
+    dev = torch._C._cuda_getDevice()
+    bf16, u8 = torch.bfloat16, torch.uint8
+    c_layer = _FfnLayer(_dense(gate_up, u8, dev), _dense(down, u8, dev), _dense(agu, bf16, dev), _dense(zgu, bf16, dev),
+                        _dense(adn, bf16, dev), _dense(zdn, bf16, dev), r)
     flags = (MQ_FLAG_FFN_SILU if silu else 0) | (MQ_FLAG_FFN_RESIDUAL if residual else 0)
-    st = _lib.mq_experts_ffn(_ptr(x, torch.bfloat16), ctypes.byref(c_layer), _ptr(ids, torch.int32), _ptr(weight, torch.float32), B, top, E, d, F,
-                             group, flags, _ptr(y, torch.bfloat16), _ptr(ws, torch.uint8), ws.numel(), _stream())
-    _check(st, "mq_experts_ffn")
+    st = _lib.mq_experts_ffn(_dense(x, bf16, dev), c_layer, _dense(ids, torch.int32, dev), _dense(weight, torch.float32, dev), B, top, E, d, F,
+                             group, flags, _dense(y, bf16, dev), _dense(ws, u8, dev), ws.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    if st:
+        _check(st, "mq_experts_ffn")
     return y

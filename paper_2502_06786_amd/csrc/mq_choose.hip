@@ -23,7 +23,8 @@ struct ChooseBwdArgs {
 // Over the LPT neighbouring lanes of a token; every lane gets the result, in the same bits.
 template <int LPT, typename Op>
 __device__ __forceinline__ int token_reduce(int v, Op op) {
-    auto dpp = [](int x, auto ctrl) { return __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false); };
+    // (all lanes of a row take part, so nothing stands in for one that does not: the move joins the operation that uses it)
+    auto dpp = [](int x, auto ctrl) { return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, 0xF, 0xF, true); };
     if constexpr (LPT >= 2) v = op(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // the neighbour
     if constexpr (LPT >= 4) v = op(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // the other pair
     if constexpr (LPT >= 8) v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));  // the other four (half row mirrored)
@@ -33,98 +34,153 @@ __device__ __forceinline__ int token_reduce(int v, Op op) {
     return v;
 }
 template <int LPT>
-__device__ __forceinline__ float token_max(float v) {
-    return __int_as_float(token_reduce<LPT>(__float_as_int(v), [](int a, int b) { return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b))); }));
-}
-template <int LPT>
-__device__ __forceinline__ float token_sum(float v) {
-    return __int_as_float(token_reduce<LPT>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+__device__ __forceinline__ int token_max(int v) {
+    return token_reduce<LPT>(v, [](int a, int b) { return max(a, b); });
 }
 template <int LPT>
 __device__ __forceinline__ int token_min(int v) {
     return token_reduce<LPT>(v, [](int a, int b) { return min(a, b); });
 }
+template <int LPT>
+__device__ __forceinline__ float token_sum(float v) {
+    return __int_as_float(token_reduce<LPT>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
 
-// A token's scores: expert v LPT + l in value v of its lane l; -inf behind the last.  NaN counts as +inf: it is chosen first, and the
-// softmax turns the token's weights into NaN.
-template <int LPT, int V>
+// Scores in whole numbers of the same order (zeros of both signs are one score), which compare without regard to NaN.
+__device__ __forceinline__ int order_of(float v) {
+    const int b = __float_as_int(v + 0.0f);
+    return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float score_of(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7FFFFFFF)); }
+constexpr int kNone = (int)0x807FFFFFu;  // of -inf
+
+// Expert of value v of lane l of a token: neighbouring lanes hold neighbouring fours.  Ascending in v.
+template <int LPT>
+__device__ __forceinline__ int expert_of(int v, int l) {
+    return v / 4 * (4 * LPT) + l * 4 + v % 4;
+}
+
+// A token's scores, -inf behind the last.  NaN counts as +inf: it is chosen first, and the softmax turns the token's weights into NaN.
+template <int LPT, int V, int VEC>
 __device__ __forceinline__ void load_scores(const float *row, int E, int l, float (&s)[V]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = v * LPT + l < E ? row[v * LPT + l] : -INFINITY;
+    for (int v = 0; v < V; v += VEC) {
+        const int e = expert_of<LPT>(v, l);
+        if constexpr (VEC == 4) {
+            f32x4 d = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (e < E) d = *reinterpret_cast<const f32x4 *>(row + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[v + i] = d[i];
+        } else {
+            s[v] = e < E ? row[e] : -INFINITY;
+        }
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) s[v] = s[v] != s[v] ? INFINITY : s[v];
 }
 
-// The largest score is taken `top` times: the largest value over the token's lanes, then the lowest of the experts that have it.
-// LPT lanes to a token, V values to a lane.  A lane keeps the choices l, l + LPT, ... and writes them at the end.
+// how many of a token's choices a lane keeps: choice j is lane j % LPT's
 template <int LPT, int V>
+constexpr int kKept = LPT * V < 32 ? V : LPT < 32 ? 32 / LPT : 1;
+
+// `top` times the largest score is taken: the largest over the token's lanes, then the lowest of the experts that have it.  Bound by the vector unit:
+// about 50 instructions to a round of the four tokens that a wave has at E = 128.
+// LPT lanes to a token, V values to a lane, VEC of them to a load.
+template <int LPT, int V, int VEC>
 __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
-    constexpr int KEPT = (LPT * V < 32 ? LPT * V : 32) / LPT > 0 ? (LPT * V < 32 ? LPT * V : 32) / LPT : 1;
+    constexpr int KEPT = kKept<LPT, V>;
     const int l = threadIdx.x % LPT;
     const int64_t m = (int64_t)blockIdx.x * (256 / LPT) + threadIdx.x / LPT;
     if (m >= a.M) return;
     float s[V], total = 0.f;
-    load_scores<LPT, V>(a.scores + m * a.ld, a.E, l, s);
-    float most = -INFINITY;
+    int o[V];
+    load_scores<LPT, V, VEC>(a.scores + m * a.ld, a.E, l, s);
+    int most = kNone;
 #pragma unroll
-    for (int v = 0; v < V; ++v) most = fmaxf(most, s[v]);
+    for (int v = 0; v < V; ++v) {
+        o[v] = order_of(s[v]);
+        most = max(most, o[v]);
+    }
     most = token_max<LPT>(most);
-    const float base = most == -INFINITY ? 0.f : most;  // (no expert at all)
+    const float base = most == kNone ? 0.f : score_of(most);  // (no expert at all)
     if (!a.renormalize) {
 #pragma unroll
         for (int v = 0; v < V; ++v) total += expf(s[v] - base);
         total = token_sum<LPT>(total);
     }
-    int id[KEPT];
-    float w[KEPT];
+    int id[KEPT], w[KEPT];
 #pragma unroll
     for (int k = 0; k < KEPT; ++k) {
         id[k] = -1;
-        w[k] = 0.f;
+        w[k] = kNone;
         for (int j = 0; j < LPT && k * LPT + j < a.top; ++j) {
-            float best = s[0];
+            int best = o[0];
 #pragma unroll
-            for (int v = 1; v < V; ++v) best = fmaxf(best, s[v]);
+            for (int v = 1; v < V; ++v) best = max(best, o[v]);
             best = token_max<LPT>(best);
-            int e = 0x7FFFFFFF;
+            int which = V;
 #pragma unroll
-            for (int v = V - 1; v >= 0; --v) e = s[v] == best ? v * LPT + l : e;
-            e = token_min<LPT>(e);
+            for (int v = V - 1; v >= 0; --v) which = o[v] == best ? v : which;
+            const int mine = which < V ? expert_of<LPT>(which, l) : 0x7FFFFFFF, e = token_min<LPT>(mine);
+            which = mine == e ? which : V;
 #pragma unroll
-            for (int v = 0; v < V; ++v) s[v] = v * LPT + l == e ? -INFINITY : s[v];
-            const float p = expf(best - base);
-            if (a.renormalize && best != -INFINITY) total += p;
-            if (l == j && best != -INFINITY) {
+            for (int v = 0; v < V; ++v) o[v] = which == v ? kNone : o[v];
+            if (l == j && best != kNone) {
                 id[k] = e;
-                w[k] = p;
+                w[k] = best;
             }
         }
     }
+    float p[KEPT], sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) {
+        p[k] = id[k] < 0 ? 0.f : expf(score_of(w[k]) - base);
+        sum += p[k];
+    }
+    if (a.renormalize) total = token_sum<LPT>(sum);
 #pragma unroll
     for (int k = 0; k < KEPT; ++k)
         if (k * LPT + l < a.top) {
             a.ids[m * a.top + k * LPT + l] = id[k];
-            a.weight[m * a.top + k * LPT + l] = id[k] < 0 ? 0.f : w[k] / total;
+            a.weight[m * a.top + k * LPT + l] = id[k] < 0 ? 0.f : p[k] / total;
         }
 }
 
-template <int LPT, int V>
+// A lane has the choices l, l + LPT, ... of its token; each goes round all its lanes, which add it to the expert it is of.
+template <int LPT, int V, int VEC>
 __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
+    constexpr int KEPT = kKept<LPT, V>;
     const int l = threadIdx.x % LPT;
     const int64_t m = (int64_t)blockIdx.x * (256 / LPT) + threadIdx.x / LPT;
     if (m >= a.M) return;
-    const int32_t *ids = a.ids + m * a.top;
-    const float *weight = a.weight + m * a.top, *dweight = a.dweight + m * a.top;
+    int id[KEPT];
+    float w[KEPT], g[KEPT];
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) {
+        const int64_t at = m * a.top + k * LPT + l;
+        const bool there = k * LPT + l < a.top;
+        id[k] = there ? a.ids[at] : -1;
+        w[k] = there ? a.weight[at] : 0.f;
+        g[k] = there ? a.dweight[at] : 0.f;
+    }
     float p[V], up[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = up[v] = 0.f;
-    if (!a.renormalize) {
-        load_scores<LPT, V>(a.scores + m * a.ld, a.E, l, p);
-        float most = -INFINITY, total = 0.f;
+    if (!a.renormalize) load_scores<LPT, V, VEC>(a.scores + m * a.ld, a.E, l, p);
+    float mean = 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) most = fmaxf(most, p[v]);
+    for (int k = 0; k < KEPT; ++k) {
+        if (id[k] < 0 || id[k] >= a.E) id[k] = -1, w[k] = g[k] = 0.f;  // (what stands beside no choice may be anything)
+        mean = __builtin_fmaf(w[k], g[k], mean);
+    }
+    mean = token_sum<LPT>(mean);
+    if (!a.renormalize) {
+        int most = kNone;
+        float total = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) most = max(most, order_of(p[v]));
         most = token_max<LPT>(most);
-        const float base = most == -INFINITY ? 0.f : most;
+        const float base = most == kNone ? 0.f : score_of(most);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             p[v] = expf(p[v] - base);
@@ -135,28 +191,39 @@ __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p[v] *= scale;
     }
-    float mean = 0.f;
-    for (int j = 0; j < a.top; ++j) {
-        const int e = ids[j];
-        if (e >= 0 && e < a.E) mean = __builtin_fmaf(weight[j], dweight[j], mean);
-    }
-    for (int j = 0; j < a.top; ++j) {
-        const int e = ids[j];
-        if (e < 0 || e >= a.E) continue;
-        const float g = a.renormalize ? weight[j] * (dweight[j] - mean) : dweight[j];
 #pragma unroll
-        for (int v = 0; v < V; ++v) up[v] += v * LPT + l == e ? g : 0.f;
-    }
+    for (int k = 0; k < KEPT; ++k) {
+        const float mine = a.renormalize ? w[k] * (g[k] - mean) : g[k];
+        for (int j = 0; j < LPT && k * LPT + j < a.top; ++j) {
+            const int e = LPT == 1 ? id[k] : __shfl(id[k], j, LPT);
+            const float d = LPT == 1 ? mine : __shfl(mine, j, LPT);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (v * LPT + l < a.E) a.dscores[m * a.E + v * LPT + l] = a.renormalize ? up[v] : p[v] * (up[v] - mean);
+            for (int v = 0; v < V; ++v) up[v] += expert_of<LPT>(v, l) == e ? d : 0.f;
+        }
+    }
+    float *out = a.dscores + m * a.E;
+#pragma unroll
+    for (int v = 0; v < V; v += VEC) {
+        const int e = expert_of<LPT>(v, l);
+        if (e >= a.E) continue;
+        if constexpr (VEC == 4) {
+            f32x4 d;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = a.renormalize ? up[v + i] : p[v + i] * (up[v + i] - mean);
+            *reinterpret_cast<f32x4 *>(out + e) = d;
+        } else {
+            out[e] = a.renormalize ? up[v] : p[v] * (up[v] - mean);
+        }
+    }
 }
 
-// f(lanes to a token, values to a lane) for E experts
+// f(lanes to a token, values to a lane, values to a load) for E experts; vec: rows are whole 16-byte pieces
 template <typename F>
-static void by_experts(int E, F f) {
-#define MQ_CHOOSE_CASE(L_, V_) \
-    if (E <= L_ * V_) return f(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{});
+static void by_experts(int E, bool vec, F f) {
+#define MQ_CHOOSE_CASE(L_, V_)                                                                                                        \
+    if (E <= L_ * V_)                                                                                                                 \
+        return vec ? f(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{}, std::integral_constant<int, 4>{})        \
+                   : f(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{}, std::integral_constant<int, 1>{});
     MQ_CHOOSE_CASE(1, 8) MQ_CHOOSE_CASE(4, 4) MQ_CHOOSE_CASE(8, 4) MQ_CHOOSE_CASE(16, 4) MQ_CHOOSE_CASE(16, 8)
     MQ_CHOOSE_CASE(32, 8) MQ_CHOOSE_CASE(64, 8) MQ_CHOOSE_CASE(64, 16)
 #undef MQ_CHOOSE_CASE
@@ -183,9 +250,9 @@ extern "C" mq_status mq_experts_choose(const float *scores, int64_t M, int64_t E
     if (!aligned16(ids) || !aligned16(weight)) return MQ_ERR_ALIGN;
     const ChooseArgs a{scores, ld, ids, weight, (int)M, (int)E, (int)top, (flags & MQ_FLAG_RENORMALIZE) != 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    by_experts((int)E, [&](auto L, auto V) {
+    by_experts((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
         constexpr int per = 256 / decltype(L)::value;
-        choose_kernel<decltype(L)::value, decltype(V)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
+        choose_kernel<decltype(L)::value, decltype(V)::value, decltype(Vec)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
     });
     return launch_status();
 }
@@ -199,9 +266,9 @@ extern "C" mq_status mq_experts_choose_bwd(const float *scores, int64_t ld, cons
     if (!aligned16(ids) || !aligned16(weight) || !aligned16(dweight) || !aligned16(dscores)) return MQ_ERR_ALIGN;
     const ChooseBwdArgs a{scores, ld, ids, weight, dweight, dscores, (int)M, (int)E, (int)top, (flags & MQ_FLAG_RENORMALIZE) != 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    by_experts((int)E, [&](auto L, auto V) {
+    by_experts((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
         constexpr int per = 256 / decltype(L)::value;
-        choose_bwd_kernel<decltype(L)::value, decltype(V)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
+        choose_bwd_kernel<decltype(L)::value, decltype(V)::value, decltype(Vec)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
     });
     return launch_status();
 }
