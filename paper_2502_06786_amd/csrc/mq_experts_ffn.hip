@@ -16,9 +16,9 @@
 
 namespace mq {
 
-// waves of a workgroup at most: 16 leave 128 registers to each
-constexpr int gate_up_waves(int R, int MOST) { return 8; }
-constexpr int down_waves(int R, int RG, int MOST) { return 12; }
+// waves of a workgroup at most: 8 leave 256 registers to each, 12 168
+constexpr int kGateUpWaves = 8;
+constexpr int down_waves(int R) { return R == 2 ? 8 : 12; }
 constexpr int kFfnTop = 16, kFfnChoices = kGroupedTokens * kFfnTop;
 
 struct ExpertsFfnArgs {
@@ -57,7 +57,7 @@ __device__ __forceinline__ int take_from(int from, int v) { return __builtin_amd
 
 // MOST: tokens that an expert may have, 4, 8 or 16
 template <int R, int C, int RG, int MOST, int D>
-__global__ __launch_bounds__(64 * gate_up_waves(R, MOST)) void experts_gate_up_kernel(ExpertsFfnArgs a) {
+__global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
     const int choice = blockIdx.y, e = a.ids[choice];
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * gate_up_waves(R, MOST)) void experts_gate_up_k
         int at = wave;
         uint32_t begin[G::XI];
 #pragma unroll
-        for (int i = 0; i < G::XI; ++i) begin[i] = (uint32_t)(take_from(min(load_token<G>(i), count - 1), token) * a.d);
+        for (int i = 0; i < G::XI; ++i) begin[i] = 2 * (uint32_t)(take_from(min(load_token<G>(i), count - 1), token) * a.d);
         grouped_stream<R, C, RG, T, false, decltype(ahead)::value>(
             lds + wave * Grouped<R, C, RG, MOST>::LDS, 2 * a.F - row0, a.d, a.groups_d, a.group, y,
             [&](Stretch<G::XI> &s) {
@@ -154,7 +154,7 @@ struct DownLds {
 
 // MOST: tokens of an entry, 4 or 8.  blockIdx.y: which of the workgroups that share the rows
 template <int R, int C, int RG, int MOST, int D>
-__global__ __launch_bounds__(64 * down_waves(R, RG, MOST)) void experts_down_kernel(ExpertsFfnArgs a) {
+__global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     using Lds = DownLds<R, C, RG, MOST>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * down_waves(R, RG, MOST)) void experts_down_ker
 #pragma unroll
                 for (int i = 0; i < G::XI; ++i) {
                     const int t = load_token<G>(i) % (2 * TOKENS);
-                    s.token[i] = (uint32_t)a.row[entry * 8 + min(t % TOKENS, s.count - 1)] * (uint32_t)a.F + (t < TOKENS ? 0u : rest);
+                    s.token[i] = 2 * ((uint32_t)a.row[entry * 8 + min(t % TOKENS, s.count - 1)] * (uint32_t)a.F + (t < TOKENS ? 0u : rest));
                 }
                 s.first = (item - which * stretches) * kPieces * kHalves;
                 s.tokens = *reinterpret_cast<const uint32_t *>(a.token + entry * 8 + 4 * (quarter & 1));
@@ -290,7 +290,7 @@ template <int R, int C, int RG, int MOST, int D>
 mq_status launch_gate_up_as(ExpertsFfnArgs a, hipStream_t st) {
     constexpr int LDS = Grouped<R, C, RG, MOST>::LDS;
     const int64_t stretches = cdiv(a.d, kStretchCodes<R>), blocks = cdiv(2 * a.F, kGroupedRows * RG);
-    a.ks = (int)std::min<int64_t>({stretches, gate_up_waves(R, MOST), 163840 / LDS, cdiv(6144, blocks * std::min(a.n, a.E))});
+    a.ks = (int)std::min<int64_t>({stretches, kGateUpWaves, 163840 / LDS, cdiv(6144, blocks * std::min(a.n, a.E))});
     a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
     const int lds = a.ks * LDS;
     constexpr auto kernel = experts_gate_up_kernel<R, C, RG, MOST, D>;
@@ -304,7 +304,7 @@ mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
     const int64_t items = cdiv(a.F, kStretchCodes<R>) * std::min(a.n, a.E), blocks = cdiv(a.d, kGroupedRows * RG);
     // a workgroup for each compute unit, of as many waves as there are items and room
     a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kDownSplits, 256 / blocks, items / 8}));
-    const int waves = (int)std::min<int64_t>({cdiv(items, a.splits), down_waves(R, RG, MOST), (163840 - Lds::LIST) / Lds::WAVE});
+    const int waves = (int)std::min<int64_t>({cdiv(items, a.splits), down_waves(R), (163840 - Lds::LIST) / Lds::WAVE});
     const int lds = Lds::LIST + waves * Lds::WAVE;
     constexpr auto kernel = experts_down_kernel<R, C, RG, MOST, D>;
     if (lds > 65536 && !allow_lds<kernel>(lds)) return MQ_ERR_DEVICE;
@@ -313,14 +313,17 @@ mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
 }
 template <int R, int C, int MOST>
 mq_status launch_gate_up(const ExpertsFfnArgs &a, hipStream_t st) {
-    // two tiles to a wave where that leaves enough waves (at two bits it leaves too few registers)
-    if (R != 2 && cdiv(2 * a.F, 2 * kGroupedRows) * std::min(a.n, a.E) >= 2048) return launch_gate_up_as<R, C, 2, MOST, 2>(a, st);
-    return launch_gate_up_as<R, C, 1, MOST, 2>(a, st);
+    // Two tiles to a wave, which share the tokens' way through LDS, where that leaves enough waves; a piece under way beside the one that is
+    // multiplied, but at two bits, which are bound by the vector unit and want registers for more waves.
+    constexpr int D = R == 2 ? 1 : 2;
+    if (cdiv(2 * a.F, 2 * kGroupedRows) * std::min(a.n, a.E) >= 2048) return launch_gate_up_as<R, C, 2, MOST, D>(a, st);
+    return launch_gate_up_as<R, C, 1, MOST, D>(a, st);
 }
 template <int R, int C, int MOST>
 mq_status launch_down(const ExpertsFfnArgs &a, hipStream_t st) {
-    if (cdiv(a.d, 2 * kGroupedRows) * std::min(a.n, a.E) * cdiv(a.F, kStretchCodes<R>) >= 2048) return launch_down_as<R, C, 2, MOST, R == 2 ? 1 : 2>(a, st);
-    return launch_down_as<R, C, 1, MOST, R == 2 ? 1 : 2>(a, st);
+    constexpr int D = R == 2 || (R == 4 && C == 32) ? 1 : 2;
+    if (cdiv(a.d, 2 * kGroupedRows) * std::min(a.n, a.E) * cdiv(a.F, kStretchCodes<R>) >= 2048) return launch_down_as<R, C, 2, MOST, D>(a, st);
+    return launch_down_as<R, C, 1, MOST, D>(a, st);
 }
 template <int R, int C>
 mq_status launch_half(const ExpertsFfnArgs &a, bool down, hipStream_t st) {

@@ -9,8 +9,9 @@ namespace mq {
 // y[t, n] = sum over groups of alpha (2^s sum code x - z sum x).  A wave takes tiles of 16 rows of the plane (the matrix core's columns: lane
 // & 15) and up to 16 tokens (its rows), 32 codes to a step.  Two products run side by side: tokens x codes and tokens x ones, whose result is
 // sum x in the very lanes that hold the tokens' products; both are whole sums in fp32 over a chunk (a part of one group) before they meet
-// alpha and z.  Codes of 4 and 2 bits enter as 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of
-// them), which sum x takes out again.
+// alpha and z.  Codes of 4 bits enter as 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of them), which
+// sum x takes out again.  Two bits at mantissa bits 0, 2 or 4 under the exponent of 128, 32 or 8 are such numbers too, so codes of 2 bits need two
+// shifts to a register instead of seven; a third product, of the tokens with the negative of these, stands in the sums before the codes do.
 //
 // Memory is read in pieces of a row, its 128-byte lines, by eight neighbouring lanes (and tokens alike): lanes that lie apart cost the address unit a
 // cycle each, 64 for a load whose lanes are all in different rows.  A wave's own part of LDS turns pieces into the matrix core's operands; pieces under
@@ -20,8 +21,9 @@ namespace mq {
 // mask leaves.
 constexpr int kGroupedTokens = 16, kGroupedRows = 16;
 
+// what sum x takes out of the products
 template <int R>
-constexpr float kCodeOffset = R == 8 ? 0.0f : 128.0f;
+constexpr float kCodeOffset = R == 4 ? 128.0f : 0.0f;
 
 // place of input k of a row that is stored in operand order
 template <int R>
@@ -72,7 +74,7 @@ struct Grouped {
     static constexpr int XS = PC / 8;                                // 16-byte slots of a token in half a piece
     static constexpr int XI = T * XS < 64 ? 1 : T * XS / 64;         // loads of them for a wave
     static constexpr int CODES = RG * 2048, TOKENS = XI * 1024;      // bytes of LDS
-    static constexpr int LDS = CODES + TOKENS + RG * 4 * NC * 64;
+    static constexpr int LDS = CODES + TOKENS + RG * 4 * NC * 128;
 };
 
 // A stretch of a product that one wave does: two pieces of 16 RG rows.  Bases are the same for the whole wave.
@@ -81,7 +83,7 @@ struct Stretch {
     const uint8_t *codes;          // row 0 of the tiles, code 0 of the rows
     const uint16_t *alpha, *zero;  // row 0 of the tiles, group 0
     const uint16_t *x;
-    uint32_t token[XI];            // begin of the token that a lane loads for (values, from x)
+    uint32_t token[XI];            // begin of the token that a lane loads for (bytes, from x)
     int first;                     // first half piece
     // the layer's down product: whose outputs a lane's y are
     int count;                     // tokens
@@ -106,13 +108,16 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // (places in LDS are computed here, for each stream anew, instead of being kept in registers around it)
     const int li = lane & 15, quarter = lane >> 4, part = lane & 3;
-    const int bytes = K / 8 * R, chunks = K / C;
+    const int bytes = K / 8 * R, chunks = K / C, halves = (K + PC - 1) / PC;
     const float step = (float)(1 << (8 - R));
     const u32x4 ones{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-    uint32_t mask = R == 4 ? 0x000F000Fu : 0x00030003u, base = 0x43004300u;  // (in registers: one instruction for "and" and "or", which takes no two literals)
-    asm volatile("" : "+s"(mask), "+v"(base));
+    // (in registers: one instruction for "and" and "or", which takes no two literals)
+    uint32_t mask[3] = {R == 4 ? 0x000F000Fu : 0x00030003u, 0x000C000Cu, 0x00300030u}, base[3] = {0x43004300u, 0x42004200u, 0x41004100u};
+    asm volatile("" : "+s"(mask[0]), "+s"(mask[1]), "+s"(mask[2]), "+v"(base[0]), "+v"(base[1]), "+v"(base[2]));
+    // code pair j of a register of 2-bit codes stands at position j % 3 after a shift by 6 (j / 3)
+    const u32x4 minus[2] = {{0xC300C300u, 0xC200C200u, 0xC100C100u, 0xC300C300u}, {0xC200C200u, 0xC100C100u, 0xC300C300u, 0xC200C200u}};
     uint8_t *const lds_x = lds + G::CODES;
-    uint32_t *const lds_params = reinterpret_cast<uint32_t *>(lds_x + G::TOKENS);
+    f32pair_t *const lds_params = reinterpret_cast<f32pair_t *>(lds_x + G::TOKENS);  // what a chunk's two sums are multiplied with
 
     uint32_t row_codes[RG][2], row_params[RG];
 #pragma unroll
@@ -144,8 +149,8 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
         for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int i = 0; i < XI; ++i) {
-                const uint32_t v = s.token[i] + (uint32_t)min((s.first + kHalves * j + h) * PC + (64 * i + lane) % XS * 8, K - 8);
-                x[slot][h][i] = *reinterpret_cast<const u32x4 *>(s.x + v);
+                const uint32_t v = s.token[i] + 2 * (uint32_t)min((s.first + kHalves * j + h) * PC + (64 * i + lane) % XS * 8, K - 8);
+                x[slot][h][i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(s.x) + v);
             }
     };
     auto fetch_params = [&](const Stretch<XI> &s) {
@@ -200,11 +205,14 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
                     if constexpr (R == 4) {
                         const uint32_t d = *reinterpret_cast<const uint32_t *>(tile + (((4 * h + k) ^ codes_turn) << 4) + 4 * quarter);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] = ((d >> (4 * i)) & mask) | base;
+                        for (int i = 0; i < 4; ++i) o[i] = ((d >> (4 * i)) & mask[0]) | base[0];
                     } else if constexpr (R == 2) {
                         if (!(k & 1)) both[t] = *reinterpret_cast<const uint32_t *>(tile + (((4 * h + (k >> 1)) ^ codes_turn) << 4) + 4 * quarter);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] = ((both[t] >> (8 * (k & 1) + 2 * i)) & mask) | base;
+                        for (int i = 0; i < 4; ++i) {
+                            const int j = 4 * (k & 1) + i;
+                            o[i] = ((both[t] >> (6 * (j / 3))) & mask[j % 3]) | base[j % 3];
+                        }
                     } else {
                         const u32x2 d = *reinterpret_cast<const u32x2 *>(tile + (((4 * h + 2 * k + (quarter >> 1)) ^ codes_turn) << 4) + 8 * (quarter & 1));
 #pragma unroll
@@ -213,17 +221,16 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
                             o[i] = halves_hi(__float_as_uint(lo), __float_as_uint(hi));
                         }
                     }
+                    if constexpr (R == 2) dot[t] = mfma_tokens(v, minus[k & 1], dot[t]);
                     dot[t] = mfma_tokens(v, o, dot[t]);
                 }
             }
             const int chunk = half * NC + c;
 #pragma unroll
             for (int t = 0; t < RG; ++t) {
-                const uint32_t az = lds_params[(t * 4 * NC + chunk) * 16 + li];
-                const float a = s.first * NC + chunk < chunks ? bf16_lo(az) : 0.f;
-                const float scale = a * step, shift = a * __builtin_fmaf(step, kCodeOffset<R>, bf16_hi(az));
+                const f32pair_t by = lds_params[(t * 4 * NC + chunk) * 16 + li];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[t][i] = __builtin_fmaf(scale, dot[t][i], __builtin_fmaf(-shift, sum[i], y[t][i]));
+                for (int i = 0; i < 4; ++i) y[t][i] = __builtin_fmaf(by[0], dot[t][i], __builtin_fmaf(by[1], sum[i], y[t][i]));
                 asm volatile("" : "+v"(y[t]));  // (done here: put off to where y is used, every chunk's sums would stay in registers)
             }
         }
@@ -241,12 +248,17 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
 #pragma unroll
         for (int t = 0; t < RG; ++t)
 #pragma unroll
-            for (int i = 0; i < NC; ++i) lds_params[(t * 4 * NC + 4 * i + part) * 16 + (lane >> 2)] = (uint32_t)alpha[t][i] | (uint32_t)zero[t][i] << 16;
+            for (int i = 0; i < NC; ++i) {
+                const float a = s.first * NC + 4 * i + part < chunks ? bf16_bits_to_float(alpha[t][i]) : 0.f;
+                lds_params[(t * 4 * NC + 4 * i + part) * 16 + (lane >> 2)] =
+                    f32pair_t{a * step, -a * __builtin_fmaf(step, kCodeOffset<R>, bf16_bits_to_float(zero[t][i]))};
+            }
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) {
-                multiply(s, kHalves * j + h, j % D);
+                // (a row's end, where there may be less, comes last)
+                if (decltype(with_next)::value || kHalves * j + h == 0 || s.first + kHalves * j + h < halves) multiply(s, kHalves * j + h, j % D);
                 __builtin_amdgcn_sched_barrier(0);  // (keeps the requests of later pieces and what unpacks them out of this one's registers)
             }
             if (j + D < kPieces) {

@@ -14,12 +14,14 @@ struct GroupedGemvArgs {
     GroupOf group;
 };
 
-// waves of a workgroup at most: 16 leave 128 registers to each
-constexpr int gemv_waves(int R, int RG, int T, int D) { return R == 2 && (T == 16 || RG * D == 4) ? 8 : 16; }
+// waves of a workgroup at most: 16 leave 128 registers to each, 8 256
+constexpr int gemv_waves(int R, int C, int RG, int T, int D) {
+    return (R == 2 && (T == 16 || RG * D == 4)) || (R == 4 && C == 32 && RG == 2) ? 8 : 16;
+}
 
 // A workgroup takes 16 RG rows, its waves stretches of them in turn; the waves' sums meet in LDS.
 template <int R, int C, int RG, int T, int D>
-__global__ __launch_bounds__(64 * gemv_waves(R, RG, T, D)) void gemv_grouped_kernel(GroupedGemvArgs a) {
+__global__ __launch_bounds__(64 * gemv_waves(R, C, RG, T, D)) void gemv_grouped_kernel(GroupedGemvArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     using G = Grouped<R, C, RG, T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
@@ -37,7 +39,7 @@ __global__ __launch_bounds__(64 * gemv_waves(R, RG, T, D)) void gemv_grouped_ker
             s.zero = a.zero + (int64_t)row0 * a.groups;
             s.x = a.x;
 #pragma unroll
-            for (int i = 0; i < G::XI; ++i) s.token[i] = (uint32_t)(min(load_token<G>(i), a.B - 1) * a.K);
+            for (int i = 0; i < G::XI; ++i) s.token[i] = 2 * (uint32_t)(min(load_token<G>(i), a.B - 1) * a.K);
             s.first = at * kPieces * kHalves;
             at += a.ks;
             return true;
@@ -72,7 +74,7 @@ static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
     // Waves of a workgroup: 12 on each compute unit where there is no more than a workgroup or two for each (4096 x 14336, B = 16: 11.8 us, with
     // 14 waves instead of 10 12.9), otherwise 24, of which 16 to 20 are there at a time (73728 x 4608, B = 1: 34.9 us, half as many 39.4).
     const int64_t wanted = cdiv(blocks <= 512 ? 3072 : 6144, blocks);
-    a.ks = (int)std::min<int64_t>({stretches, gemv_waves(R, RG, T, D), 163840 / G::LDS, wanted});
+    a.ks = (int)std::min<int64_t>({stretches, gemv_waves(R, C, RG, T, D), 163840 / G::LDS, wanted});
     a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
     const int lds = a.ks * G::LDS;
     constexpr auto kernel = gemv_grouped_kernel<R, C, RG, T, D>;
