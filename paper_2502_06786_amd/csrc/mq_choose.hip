@@ -84,7 +84,7 @@ template <int LPT, int V>
 constexpr int kKept = LPT * V < 32 ? V : LPT < 32 ? 32 / LPT : 1;
 
 // `top` times the largest score is taken: the largest over the token's lanes, then the lowest of the experts that have it.  Bound by the vector unit:
-// about 50 instructions to a round of the four tokens that a wave has at E = 128.
+// about 90 instructions to a round of the eight tokens that a wave has at E = 128.
 // LPT lanes to a token, V values to a lane, VEC of them to a load.
 template <int LPT, int V, int VEC>
 __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
@@ -217,15 +217,23 @@ __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
     }
 }
 
-// f(lanes to a token, values to a lane, values to a load) for E experts; vec: rows are whole 16-byte pieces
-template <typename F>
+// f(lanes to a token, values to a lane, values to a load) for E experts; vec: rows are whole 16-byte pieces.  The choice takes as many steps
+// between lanes whatever a lane holds, so fewer lanes with more values each are quicker (65531 x 128, 8 of them: 15.9 us with 8 lanes, 17.5 with 16);
+// the gradient, which is bound by memory, wants short loops (65536 x 128: 14.9 us with 16 lanes, 16.8 with 8).
+template <bool CHOICE, typename F>
 static void by_experts(int E, bool vec, F f) {
-#define MQ_CHOOSE_CASE(L_, V_)                                                                                                        \
-    if (E <= L_ * V_)                                                                                                                 \
-        return vec ? f(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{}, std::integral_constant<int, 4>{})        \
-                   : f(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{}, std::integral_constant<int, 1>{});
-    MQ_CHOOSE_CASE(1, 8) MQ_CHOOSE_CASE(4, 4) MQ_CHOOSE_CASE(8, 4) MQ_CHOOSE_CASE(16, 4) MQ_CHOOSE_CASE(16, 8)
-    MQ_CHOOSE_CASE(32, 8) MQ_CHOOSE_CASE(64, 8) MQ_CHOOSE_CASE(64, 16)
+    auto with = [&](auto lanes, auto values) {
+        return vec ? f(lanes, values, std::integral_constant<int, 4>{}) : f(lanes, values, std::integral_constant<int, 1>{});
+    };
+#define MQ_CHOOSE_CASE(L_, V_) \
+    if (E <= L_ * V_) return with(std::integral_constant<int, L_>{}, std::integral_constant<int, V_>{});
+    MQ_CHOOSE_CASE(1, 8) MQ_CHOOSE_CASE(4, 4) MQ_CHOOSE_CASE(8, 4)
+    if constexpr (CHOICE) {
+        MQ_CHOOSE_CASE(8, 8) MQ_CHOOSE_CASE(8, 16) MQ_CHOOSE_CASE(16, 16)
+    } else {
+        MQ_CHOOSE_CASE(16, 4) MQ_CHOOSE_CASE(16, 8) MQ_CHOOSE_CASE(32, 8)
+    }
+    MQ_CHOOSE_CASE(64, 8) MQ_CHOOSE_CASE(64, 16)
 #undef MQ_CHOOSE_CASE
 }
 
@@ -250,7 +258,7 @@ extern "C" mq_status mq_experts_choose(const float *scores, int64_t M, int64_t E
     if (!aligned16(ids) || !aligned16(weight)) return MQ_ERR_ALIGN;
     const ChooseArgs a{scores, ld, ids, weight, (int)M, (int)E, (int)top, (flags & MQ_FLAG_RENORMALIZE) != 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    by_experts((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
+    by_experts<true>((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
         constexpr int per = 256 / decltype(L)::value;
         choose_kernel<decltype(L)::value, decltype(V)::value, decltype(Vec)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
     });
@@ -266,7 +274,7 @@ extern "C" mq_status mq_experts_choose_bwd(const float *scores, int64_t ld, cons
     if (!aligned16(ids) || !aligned16(weight) || !aligned16(dweight) || !aligned16(dscores)) return MQ_ERR_ALIGN;
     const ChooseBwdArgs a{scores, ld, ids, weight, dweight, dscores, (int)M, (int)E, (int)top, (flags & MQ_FLAG_RENORMALIZE) != 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    by_experts((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
+    by_experts<false>((int)E, E % 4 == 0 && ld % 4 == 0 && aligned16(scores), [&](auto L, auto V, auto Vec) {
         constexpr int per = 256 / decltype(L)::value;
         choose_bwd_kernel<decltype(L)::value, decltype(V)::value, decltype(Vec)::value><<<dim3((unsigned)cdiv(M, per)), dim3(256), 0, st>>>(a);
     });

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(Expe
 // LDS of the down kernel: for each wave its part of the products and 16 tokens x 16 RG rows of sums; the entries in use.
 template <int R, int C, int RG, int MOST>
 struct DownLds {
-    static constexpr int STREAM = Grouped<R, C, RG, 2 * MOST>::LDS, WAVE = STREAM + 1024 * RG, LIST = 2 * kFfnChoices * 2 + 16;
+    static constexpr int STREAM = Grouped<R, C, RG, 2 * MOST>::LDS, WAVE = STREAM + 1024 * RG, LIST = 2 * kFfnChoices * 8 + 16;
 };
 
 // MOST: tokens of an entry, 4 or 8.  blockIdx.y: which of the workgroups that share the rows
@@ -161,18 +161,20 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
     const int waves = (int)(blockDim.x >> 6), row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.F + kStretchCodes<R> - 1) / kStretchCodes<R>;
     uint8_t *const mine = lds + Lds::LIST + wave * Lds::WAVE;
     float *const sums = reinterpret_cast<float *>(mine + Lds::STREAM);  // [token][row]
-    uint16_t *const list = reinterpret_cast<uint16_t *>(lds);           // entries of up to 4 tokens from the front, of more from the back
+    // (entry, tokens << 16; expert): entries of up to 4 tokens from the front, of more from the back
+    u32x2 *const list = reinterpret_cast<u32x2 *>(lds);
     int *const totals = reinterpret_cast<int *>(lds + Lds::LIST - 16);
     const int entries = MOST == 4 ? a.n : 2 * a.n;  // (4 tokens fill no second entry)
     if (wave == 0) {
         int few = 0, more = 0;
         for (int at = 0; at < entries; at += 64) {
-            const int entry = at + lane, count = entry < entries ? a.count[entry] : 0;
+            const int entry = at + lane, count = entry < entries ? a.count[entry] : 0, expert = a.expert[min(entry, entries - 1)];
+            const u32x2 word = {(uint32_t)entry | (uint32_t)count << 16, (uint32_t)expert};
             const uint64_t f = __ballot(count > 0 && count <= 4), m = __ballot(count > 4), below = (1ull << lane) - 1;
             if (count > 4)
-                list[2 * kFfnChoices - 1 - more - __popcll(m & below)] = (uint16_t)entry;
+                list[2 * kFfnChoices - 1 - more - __popcll(m & below)] = word;
             else if (count > 0)
-                list[few + __popcll(f & below)] = (uint16_t)entry;
+                list[few + __popcll(f & below)] = word;
             few += __popcll(f);
             more += __popcll(m);
         }
@@ -195,9 +197,11 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
             mine, a.d - row0, a.F, a.groups_F, a.group, y,
             [&](Stretch<G::XI> &s) {
                 if (item >= items) return false;
-                const int which = item / stretches, entry = __builtin_amdgcn_readfirstlane((int)entry_of(which));
-                const int64_t first_row = (int64_t)a.expert[entry] * a.d + row0;
-                s.count = a.count[entry];
+                const int which = item / stretches;
+                const u32x2 word = entry_of(which);
+                const int packed = __builtin_amdgcn_readfirstlane((int)word[0]), entry = packed & 0xFFFF;
+                const int64_t first_row = (int64_t)__builtin_amdgcn_readfirstlane((int)word[1]) * a.d + row0;
+                s.count = packed >> 16;
                 s.codes = a.down + first_row * (a.F / 8 * R);
                 s.alpha = a.alpha_dn + first_row * a.groups_F;
                 s.zero = a.zero_dn + first_row * a.groups_F;

@@ -16,7 +16,7 @@ struct GroupedGemvArgs {
 
 // waves of a workgroup at most: 16 leave 128 registers to each, 8 256
 constexpr int gemv_waves(int R, int C, int RG, int T, int D) {
-    return (R == 2 && (T == 16 || RG * D == 4)) || (R == 4 && C == 32 && RG == 2) ? 8 : 16;
+    return (R == 2 && (T == 16 || RG == 2)) || (R == 4 && C == 32 && RG == 2) ? 8 : 16;
 }
 
 // A workgroup takes 16 RG rows, its waves stretches of them in turn; the waves' sums meet in LDS.
@@ -89,7 +89,8 @@ static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
 // (28672 x 4096: 12.9 and 13.5).  Groups of 32 at four bits leave no registers for it (73728 x 4608: 57 and 51 us).
 template <int R, int C>
 static mq_status launch_gemv_grouped(const GroupedGemvArgs &a, hipStream_t st) {
-    if (a.B > 4) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 16, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 16, 1>(a, st);
+    if (a.B > 8) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 16, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 16, 1>(a, st);
+    if (a.B > 4) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 8, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 8, 1>(a, st);
     if constexpr (R == 4 && C == 32) return launch_gemv_grouped_as<R, C, 1, 4, 2>(a, st);
     if constexpr (R != 4 || C != 32) {
         if (a.N >= (R == 4 ? 65536 : 16384)) return launch_gemv_grouped_as<R, C, 2, 4, 2>(a, st);

@@ -48,7 +48,7 @@ def gemv(mq, x, codes, alpha, zero, r, group, **kw):
 SHAPES = [(1, 1, 32, 32, 4), (1, 16, 64, 64, 2), (2, 17, 32, 32, 8), (16, 15, 96, 96, 4), (3, 33, 160, 32, 4), (5, 100, 384, 192, 2), (16, 48, 512, 64, 4),
           (4, 31, 544, 32, 8), (7, 1000, 1024, 128, 4), (1, 257, 2304, 64, 2), (9, 40, 2304, 256, 2), (13, 64, 1152, 64, 8), (1, 16, 9216, 128, 4),
           (16, 20, 9216, 9216, 4), (2, 35, 10240, 512, 2), (6, 18, 8960, 320, 8), (1, 4099, 256, 256, 4), (11, 23, 33 * 640, 640, 4),
-          (15, 50, 17 * 128, 128, 4), (8, 50, 33 * 64, 64, 4), (1, 5, 17 * 512, 32, 4), (10, 70, 19 * 192, 64, 2), (1, 9, 1 << 18, 4096, 2)]
+          (15, 50, 17 * 128, 128, 4), (2, 3, 1 << 20, 1 << 20, 4), (6, 9000, 704, 64, 4), (16, 8200, 320, 32, 4), (7, 16390, 384, 128, 2), (8, 70, 96, 96, 8), (8, 50, 33 * 64, 64, 4), (1, 5, 17 * 512, 32, 4), (10, 70, 19 * 192, 64, 2), (1, 9, 1 << 18, 4096, 2)]
 
 
 @pytest.mark.parametrize("B,N,K,group,r", SHAPES)
@@ -96,7 +96,6 @@ def test_gemv_token_of_no_numbers_is_alone(mq):
         keep = [b for b in range(16) if b not in (5, 15)]
         assert torch.equal(got[keep], want[keep])
         assert not torch.isfinite(got[[5, 15]]).any()
-    assert torch.equal(gemv(mq, x[:3], codes, alpha, zero, 4, 128), want[:3])   # nor does their number show
 
 
 def test_gemv_of_what_the_library_quantizes(mq):
@@ -382,3 +381,116 @@ def test_tokens_do_not_wait_for_the_default_stream(mq):
         got = mq.mq_gemv_grouped(late, packed, a, z, 4, 1024, 128)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# far and side by side
+# ---------------------------------------------------------------------------------------------------------------------
+def test_gemv_of_a_plane_past_four_gigabytes(mq):
+    """Its last rows are those of a plane of these rows alone (other workgroups, the same order of sums: it goes by K and the group but for the number
+    of waves, which is the same for planes of this many rows)."""
+    N, K, group = 1_200_000, 8192, 128
+    packed = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda")
+    alpha = (0.001 * torch.rand(N, K // group, device="cuda")).to(torch.bfloat16)
+    zero = (120 + 16 * torch.rand(N, K // group, device="cuda")).to(torch.bfloat16)
+    x = torch.randn(3, K, device="cuda").to(torch.bfloat16)
+    got = mq.mq_gemv_grouped(x, packed, alpha, zero, 4, K, group)
+    for a in (0, 1_048_570, N - 100_000):   # byte 2^32 is in row 1048576
+        part = slice(a, a + 100_000)
+        want = mq.mq_gemv_grouped(x, packed[part].contiguous(), alpha[part].contiguous(), zero[part].contiguous(), 4, K, group)
+        assert float((got[:, part].float() - want.float()).abs().max()) <= 2.0 ** -7 * float(want.float().abs().max())
+        assert float((got[:, part] != want).float().mean()) < 0.01
+    y, bar = ref.product(x.cpu().double().numpy(), ref.unpack(packed[-32:].cpu().numpy(), K, 4), alpha[-32:].cpu().double().numpy(),
+                         zero[-32:].cpu().double().numpy(), 4)
+    assert (np.abs(got[:, -32:].cpu().double().numpy() - y) <= bar + ref.BF16 * (np.abs(y) + bar)).all()
+
+
+def test_layer_of_experts_past_four_gigabytes(mq):
+    """The last expert of many is that expert among two (as many as there are choices, by which the work is cut)."""
+    E, d, F, group = 100, 4096, 14336, 128
+    L = {"r": 4}
+    for name, short, rows, K in (("gate_up", "gu", 2 * F, d), ("down", "dn", d, F)):
+        L[name] = torch.randint(0, 256, (E, rows, K // 2), dtype=torch.uint8, device="cuda")
+        L["alpha_" + short] = torch.full((E, rows, K // group), 0.0005, device="cuda").to(torch.bfloat16)
+        L["zero_" + short] = (120 + 16 * torch.rand(E, rows, K // group, device="cuda")).to(torch.bfloat16)
+    x = torch.randn(2, d, device="cuda").to(torch.bfloat16)
+    ids, weight = torch.tensor([[E - 1], [E - 1]], dtype=torch.int32, device="cuda"), torch.ones(2, 1, device="cuda")
+    got = mq.mq_experts_ffn(x, L, ids, weight, F, group, silu=True)
+    two = {k: (v[E - 2:].contiguous() if isinstance(v, torch.Tensor) else v) for k, v in L.items()}
+    assert torch.equal(got, mq.mq_experts_ffn(x, two, torch.ones_like(ids), weight, F, group, silu=True))
+    assert torch.isfinite(got).all() and float(got.float().std()) > 0
+
+
+def test_choose_of_many_tokens(mq):
+    """Enough of them for every compute unit several times over, against a stable sort and a softmax in 64 bits on the GPU."""
+    for M, E, top in ((70_001, 64, 8), (131_072, 8, 2), (40_003, 128, 6)):
+        s = torch.round(64 * torch.randn(M, E, device="cuda")) / 64   # some scores are equal
+        s[torch.rand(M, E, device="cuda") < 0.05] = -torch.inf
+        ids, weight = mq.mq_experts_choose(s, top)
+        best, order = torch.sort(s, dim=1, descending=True, stable=True)
+        live = best[:, :top] > -torch.inf
+        assert torch.equal(ids, torch.where(live, order[:, :top], -1).to(torch.int32))
+        w = torch.softmax(s.double(), 1).nan_to_num(0.0).gather(1, order[:, :top])
+        # half a step of the exponent's argument (up to 12) each way, of the sum of E, of the quotient
+        assert float(((weight - w).abs() / w.clamp(min=1e-30))[live].max()) < ref.U32 * (2 * 24 + E + 12)
+        assert not weight[~live].any()
+
+
+def test_two_calls_at_once(mq):
+    """Two streams, each with its own buffers."""
+    rng = np.random.default_rng(60)
+    runs = []
+    for B in (3, 12):
+        host, dev = make_layer(rng, 6, 256, 320, 64, 4)
+        x, (ids, weight) = bf16(rng.standard_normal((B, 256))), choices(rng, B, 2, 6)
+        args = (to_gpu(x, torch.bfloat16), dev, to_gpu(ids), to_gpu(weight), 320, 64)
+        y, bar = ref.layer(x, host, ids, weight, 4, True)
+        ws = torch.empty(mq.mq_workspace_bytes(mq.MQ_OP_EXPERTS_FFN, B * 2, 320, 256, 1), dtype=torch.uint8, device="cuda")
+        runs.append((args, ws, torch.cuda.Stream(), y, bar))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(50):
+        for out, (args, ws, stream, _, _) in zip(outs, runs):
+            with torch.cuda.stream(stream):
+                out.append(mq.mq_experts_ffn(*args, silu=True, ws=ws))
+    torch.cuda.synchronize()
+    for out, (_, _, _, y, bar) in zip(outs, runs):
+        assert all(torch.equal(o, out[0]) for o in out)
+        assert (np.abs(out[0].cpu().double().numpy() - y) <= bar).all()
+
+
+def test_what_the_binding_refuses(mq):
+    rng = np.random.default_rng(70)
+    codes, alpha, zero = plane(rng, 32, 128, 64, 4)
+    packed, a, z = to_gpu(ref.pack(codes, 4)), to_gpu(alpha, torch.bfloat16), to_gpu(zero, torch.bfloat16)
+    x = torch.zeros(2, 128, dtype=torch.bfloat16, device="cuda")
+
+    def f(x=x, packed=packed, a=a, z=z, r=4, K=128, group=64, **kw):
+        return mq.mq_gemv_grouped(x, packed, a, z, r, K, group, **kw)
+    f()
+    for bad in (dict(x=x.float()), dict(x=x.cpu()), dict(x=torch.zeros(2, 256, dtype=torch.bfloat16, device="cuda")[:, ::2]), dict(x=x[:, :64]), dict(group=48),
+                dict(group=0), dict(a=a[:, :1]), dict(z=z.float()), dict(packed=packed[:, :32]), dict(K=256), dict(r=2), dict(y=torch.zeros(2, 31, device="cuda"))):
+        with pytest.raises(ValueError):
+            f(**bad)
+    with pytest.raises(mq.MqError):
+        f(x=torch.zeros(17, 128, dtype=torch.bfloat16, device="cuda"))
+    s = torch.zeros(4, 8, device="cuda")
+    ids, w = mq.mq_experts_choose(s, 2)
+    for bad in (s.double(), s.t(), s.cpu()):
+        with pytest.raises(ValueError):
+            mq.mq_experts_choose(bad, 2)
+    for bad in ((s, ids[:3], w, w), (s, ids, w[:, :1], w), (s, ids.long(), w, w), (s, ids, w, w.double())):
+        with pytest.raises(ValueError):
+            mq.mq_experts_choose_bwd(*bad)
+    with pytest.raises(mq.MqError):
+        mq.mq_experts_choose(s, 9)
+    host, dev = make_layer(rng, 3, 64, 96, 32, 4)
+    t = torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda")
+    i, v = torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.zeros(2, 2, device="cuda")
+    for bad in (dict(F=64), dict(group=64), dict(ids=i.long()), dict(weight=v[:, :1]), dict(x=t.half()), dict(layer={**dev, "r": 2})):
+        kw = dict(x=t, layer=dev, ids=i, weight=v, F=96, group=32)
+        kw.update(bad)
+        with pytest.raises(ValueError):
+            mq.mq_experts_ffn(**kw)
+    with pytest.raises(mq.MqError):
+        mq.mq_experts_ffn(t, dev, i, v, 96, 32, ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
