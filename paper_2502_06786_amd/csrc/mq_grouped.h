@@ -90,6 +90,9 @@ struct Stretch {
     uint32_t tokens;               // those of components 0 .. 3, a byte each
     f32x4 share;                   // their weights
 };
+// Between what lanes of a wave leave in LDS and what others of it read there: LDS serves a wave in order, so the compiler alone has to keep it.
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Which token a lane's i-th load of half a piece is for.
 template <typename G>
 __device__ __forceinline__ int load_token(int i) {
@@ -98,8 +101,8 @@ __device__ __forceinline__ int load_token(int i) {
 
 // Does stretch after stretch: next(s) gives the wave's next one or says that there is none, end(s, more) follows each (with more, next has
 // been asked for the one behind it already); products are added to y[tile] (lane & 15 = row, component i = token 4 (lane >> 4) + i).  While a piece is
-// multiplied the D - 1 behind it are on their way; nothing is requested behind the last stretch.  ORDERED: tokens are in operand order.  What lies behind the end of rows of K
-// inputs is read as their end again and counts for nothing.
+// multiplied the D - 1 behind it are on their way; nothing is requested behind the last stretch.  ORDERED: tokens are in operand order.
+// What lies behind the end of rows of K inputs is read as their end again and counts for nothing.
 template <int R, int C, int RG, int T, bool ORDERED, int D, typename Next, typename End>
 __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, int groups, GroupOf group, f32x4 (&y)[RG], Next next, End end) {
     using G = Grouped<R, C, RG, T>;
@@ -177,6 +180,7 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
             if constexpr (!ORDERED && R == 4) v = u32x4{halves_lo(v.x, v.z), halves_hi(v.x, v.z), halves_lo(v.y, v.w), halves_hi(v.y, v.w)};
             *reinterpret_cast<u32x4 *>(lds_x + x_to[i]) = v;
         }
+        wave_fence();
         auto slot_of_x = [&](int at) { return *reinterpret_cast<const u32x4 *>(lds_x + x_from + ((at ^ x_turn) << 4)); };
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -234,6 +238,7 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
                 asm volatile("" : "+v"(y[t]));  // (done here: put off to where y is used, every chunk's sums would stay in registers)
             }
         }
+        wave_fence();
     };
     Stretch<XI> s, n;
     if (!next(s)) return;
