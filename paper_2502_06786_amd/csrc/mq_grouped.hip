@@ -73,7 +73,7 @@ static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
     const int64_t stretches = cdiv(a.K, kStretchCodes<R>), blocks = cdiv(a.N, kGroupedRows * RG);
     // Waves of a workgroup: 12 on each compute unit where there is no more than a workgroup or two for each (4096 x 14336, B = 16: 11.8 us, with
     // 14 waves instead of 10 12.9), otherwise 24, of which 16 to 20 are there at a time (73728 x 4608, B = 1: 34.9 us, half as many 39.4).
-    const int64_t wanted = cdiv(blocks <= 512 ? 3072 : 6144, blocks);
+    const int64_t wanted = cdiv((blocks <= 512 ? 12 : 24) * 256, blocks);
     a.ks = (int)std::min<int64_t>({stretches, gemv_waves(R, C, RG, T, D), 163840 / G::LDS, wanted});
     a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
     const int lds = a.ks * G::LDS;

@@ -436,6 +436,38 @@ def test_choose_of_many_tokens(mq):
         assert not weight[~live].any()
 
 
+@pytest.mark.parametrize("E,ld", [(64, 600_000_000), (61, 600_000_001)])   # whole 16-byte pieces, single scores
+def test_choose_of_rows_far_apart(mq, E, ld):
+    """Rows of which the second begins behind 2^31 bytes and the third behind 2^32."""
+    wide = torch.empty(2 * ld + E, device="cuda")
+    part = torch.as_strided(wide, (3, E), (ld, 1))
+    part.copy_(torch.randn(3, E, device="cuda"))
+    for renormalize in (False, True):
+        a, b = mq.mq_experts_choose(part, 5, renormalize=renormalize), mq.mq_experts_choose(part.contiguous(), 5, renormalize=renormalize)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        dw = torch.randn(3, 5, device="cuda")
+        assert torch.equal(mq.mq_experts_choose_bwd(part, *a, dw, renormalize=renormalize), mq.mq_experts_choose_bwd(part.contiguous(), *a, dw, renormalize=renormalize))
+
+
+def test_choose_bwd_captured(mq):
+    """A router's step of training in a graph, replayed with other scores between eager calls."""
+    s, dw = torch.randn(300, 24, device="cuda"), torch.randn(300, 4, device="cuda")
+    ids, weight, ds = torch.empty(300, 4, dtype=torch.int32, device="cuda"), torch.empty(300, 4, device="cuda"), torch.empty(300, 24, device="cuda")
+
+    def both(**kw):
+        i, w = mq.mq_experts_choose(s, 4, **{k: kw[k] for k in ("ids", "weight") if k in kw})
+        return mq.mq_experts_choose_bwd(s, i, w, dw, **{k: kw[k] for k in ("dscores",) if k in kw})
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        both(ids=ids, weight=weight, dscores=ds)
+    for turn in range(5):
+        s.normal_()
+        dw.normal_()
+        g.replay()
+        assert torch.equal(ds, both()), turn
+
+
 def test_two_calls_at_once(mq):
     """Two streams, each with its own buffers."""
     rng = np.random.default_rng(60)
