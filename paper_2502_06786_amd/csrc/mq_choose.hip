@@ -84,7 +84,8 @@ template <int LPT, int V>
 constexpr int kKept = LPT * V < 32 ? V : LPT < 32 ? 32 / LPT : 1;
 
 // `top` times the largest score is taken: the largest over the token's lanes, then the lowest of the experts that have it.  Bound by the vector unit:
-// about 90 instructions to a round of the eight tokens that a wave has at E = 128.
+// about 90 instructions to a round of the eight tokens that a wave has at E = 128 (65531 x 128, 8 of them: 14.7 us, 2.6 TB/s; to take a score out by the
+// comparison that found it, where a wave has no equal ones, costs as much as it saves: 16.3, with 15.8 for this in the same run).
 // LPT lanes to a token, V values to a lane, VEC of them to a load.
 template <int LPT, int V, int VEC>
 __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
@@ -146,7 +147,8 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
         }
 }
 
-// A lane has the choices l, l + LPT, ... of its token; each goes round all its lanes, which add it to the expert it is of.
+// A lane has the choices l, l + LPT, ... of its token; each goes round all its lanes, which add it to the expert it is of.  Bound by memory (65531 x 64, 6
+// choices: 8.9 us, 4.3 TB/s).
 template <int LPT, int V, int VEC>
 __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
     constexpr int KEPT = kKept<LPT, V>;

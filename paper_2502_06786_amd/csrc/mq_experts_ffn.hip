@@ -16,7 +16,8 @@
 
 namespace mq {
 
-// waves of a workgroup at most: 8 leave 256 registers to each, 12 168
+// waves of a workgroup at most: 8 leave 256 registers to each, 12 168 (16 leave 128, which spill: 16 tokens x 2 of 8, 4096 x 14336, r = 4:
+// 189 us, with 12 171)
 constexpr int kGateUpWaves = 8;
 constexpr int down_waves(int R) { return R == 2 ? 8 : 12; }
 constexpr int kFfnTop = 16, kFfnChoices = kGroupedTokens * kFfnTop;
@@ -55,7 +56,11 @@ __device__ __forceinline__ uint32_t mask_window(const uint64_t (&m)[4], int at, 
 __device__ __forceinline__ int send_to(int to, int v) { return __builtin_amdgcn_ds_permute(to << 2, v); }
 __device__ __forceinline__ int take_from(int from, int v) { return __builtin_amdgcn_ds_bpermute(from << 2, v); }
 
-// MOST: tokens that an expert may have, 4, 8 or 16
+// MOST: tokens that an expert may have, 4, 8 or 16.  Experts with up to 4 load no more than 4 (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us,
+// otherwise 178; x 4 of 128, 2048 x 1408: 50 and 54.5).
+// At four and eight bits bound by HBM where experts are large (the first of these layers: 499 MB in 99.8 us, 5.0 TB/s), by
+// the start of a workgroup (who chose what, first lines, 2 to 3 us) where they are small (one token x 8 of 64, 2048 x 1024: 18 MB in 7.8 us); at two
+// bits mostly by the vector unit (5 tokens x 2 of 8, 2304 x 9216: 25 to 34 us, 2.4 TB/s; about 45 instructions to 1024 codes and a load, 10 of them unpack).
 template <int R, int C, int RG, int MOST, int D>
 __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -153,6 +158,9 @@ struct DownLds {
 };
 
 // MOST: tokens of an entry, 4 or 8.  blockIdx.y: which of the workgroups that share the rows
+// One workgroup to a compute unit, three waves to a SIMD: bound by waiting (16 tokens x 2 of 8, 4096 x 14336, r = 4: 250 MB in 68 us, 3.7 TB/s, the
+// vector unit busy for 0.39 of the cycles, LDS for 0.37, the matrix core for 0.14), for small layers by start and end (one token x 8 of 64, 2048 x
+// 1024: 9 MB in 6.5 us).
 template <int R, int C, int RG, int MOST, int D>
 __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -294,7 +302,8 @@ template <int R, int C, int RG, int MOST, int D>
 mq_status launch_gate_up_as(ExpertsFfnArgs a, hipStream_t st) {
     constexpr int LDS = Grouped<R, C, RG, MOST>::LDS;
     const int64_t stretches = cdiv(a.d, kStretchCodes<R>), blocks = cdiv(2 * a.F, kGroupedRows * RG);
-    a.ks = (int)std::min<int64_t>({stretches, kGateUpWaves, 163840 / LDS, cdiv(6144, blocks * std::min(a.n, a.E))});
+    // (waves as for the product alone: 24 for each compute unit)
+    a.ks = (int)std::min<int64_t>({stretches, kGateUpWaves, 163840 / LDS, cdiv(24 * 256, blocks * std::min(a.n, a.E))});
     a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
     const int lds = a.ks * LDS;
     constexpr auto kernel = experts_gate_up_kernel<R, C, RG, MOST, D>;
@@ -306,7 +315,8 @@ template <int R, int C, int RG, int MOST, int D>
 mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
     using Lds = DownLds<R, C, RG, MOST>;
     const int64_t items = cdiv(a.F, kStretchCodes<R>) * std::min(a.n, a.E), blocks = cdiv(a.d, kGroupedRows * RG);
-    // a workgroup for each compute unit, of as many waves as there are items and room
+    // a workgroup for each compute unit, of as many waves as there are items and room (16 tokens x 4 of 128, 2048 x 1408: 50 us, with workgroups
+    // of their own rows only 78; x 2 of 8, 4096 x 14336: 168 and 209; one token x 8 of 64, 2048 x 1024: 14.0 both)
     a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kDownSplits, 256 / blocks, items / 8}));
     const int waves = (int)std::min<int64_t>({cdiv(items, a.splits), down_waves(R), (163840 - Lds::LIST) / Lds::WAVE});
     const int lds = Lds::LIST + waves * Lds::WAVE;
@@ -317,14 +327,19 @@ mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
 }
 template <int R, int C, int MOST>
 mq_status launch_gate_up(const ExpertsFfnArgs &a, hipStream_t st) {
-    // Two tiles to a wave, which share the tokens' way through LDS, where that leaves enough waves; a piece under way beside the one that is
-    // multiplied, but at two bits, which are bound by the vector unit and want registers for more waves.
+    // Two tiles to a wave, which share the tokens' way through LDS, where that leaves enough waves (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us,
+    // with one 180; 2 tokens x 4 of 64, 2048 x 768: 13.2 with one, 14.5 with two); a piece under way beside the one that is
+    // multiplied (one token x 2 of 8, 4096 x 14336: 47.2 us, without 49.7), but at two bits, which want registers for more waves (5 tokens x 2 of 8,
+    // 2304 x 9216: 55.0, with it 58.3).
     constexpr int D = R == 2 ? 1 : 2;
     if (cdiv(2 * a.F, 2 * kGroupedRows) * std::min(a.n, a.E) >= 2048) return launch_gate_up_as<R, C, 2, MOST, D>(a, st);
     return launch_gate_up_as<R, C, 1, MOST, D>(a, st);
 }
 template <int R, int C, int MOST>
 mq_status launch_down(const ExpertsFfnArgs &a, hipStream_t st) {
+    // Tiles as above (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us, with one 181; one token x 8 of 64, 2048 x 1024: 14.1 with one, 15.7 with two).
+    // A piece under way helps small layers (2 tokens x 4 of 64, 2048 x 768: 13.2 us, without 14.0), at two bits it makes no odds (16 tokens x 2 of 8,
+    // 4096 x 14336: 155.8, without 153.9; 5 tokens x 2 of 8, 2304 x 9216: 53.6 and 55.2), groups of 32 at four bits leave no registers for it.
     constexpr int D = R == 2 || (R == 4 && C == 32) ? 1 : 2;
     if (cdiv(a.d, 2 * kGroupedRows) * std::min(a.n, a.E) * cdiv(a.F, kStretchCodes<R>) >= 2048) return launch_down_as<R, C, 2, MOST, D>(a, st);
     return launch_down_as<R, C, 1, MOST, D>(a, st);
@@ -363,8 +378,8 @@ extern "C" mq_status mq_experts_ffn(const uint16_t *x, const mq_ffn_layer *layer
     ExpertsFfnArgs a{x, ids, weight, layer->gate_up, layer->down, layer->alpha_gu, layer->zero_gu, layer->alpha_dn, layer->zero_dn, y,
                      reinterpret_cast<uint16_t *>(base + l.act), reinterpret_cast<uint16_t *>(base + l.rest), reinterpret_cast<int32_t *>(base + l.count),
                      reinterpret_cast<int32_t *>(base + l.expert), base + l.token, reinterpret_cast<int32_t *>(base + l.row),
-                     reinterpret_cast<float *>(base + l.share), reinterpret_cast<float *>(base + l.part), reinterpret_cast<uint32_t *>(base + l.arrived), (int)B, (int)top, (int)(B * top), (int)E, (int)d, (int)F,
-                     (int)(group ? d / group : 1), (int)(group ? F / group : 1), 1, 1, GroupOf{0, 0}, (flags & MQ_FLAG_FFN_SILU) != 0,
+                     reinterpret_cast<float *>(base + l.share), reinterpret_cast<float *>(base + l.part), reinterpret_cast<uint32_t *>(base + l.arrived),
+                     (int)B, (int)top, (int)(B * top), (int)E, (int)d, (int)F, (int)(group ? d / group : 1), (int)(group ? F / group : 1), 1, 1, GroupOf{0, 0}, (flags & MQ_FLAG_FFN_SILU) != 0,
                      (flags & MQ_FLAG_FFN_RESIDUAL) != 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     for (int down = 0; down < 2; ++down) {
