@@ -277,6 +277,25 @@ def test_layer_of_an_expert_chosen_twice(mq):
     check_layer(mq, x, host, dev, ids, rng.standard_normal((4, 3)).astype(np.float32), 64, 64, 4, False, False)
 
 
+@pytest.mark.parametrize("B,top,E,r", [(8, 1, 1, 4), (9, 1, 1, 4), (16, 1, 1, 2), (16, 16, 1, 4), (16, 2, 2, 8), (12, 3, 1, 2)])
+def test_layer_of_experts_that_everybody_chose(mq, B, top, E, r):
+    """Up to 16 tokens to an expert: one entry of them, one and a token, two full ones; choices of the same expert add up."""
+    rng = np.random.default_rng(24 + B)
+    host, dev = make_layer(rng, E, 128, 192, 64, r)
+    x, (ids, weight) = bf16(rng.standard_normal((B, 128))), choices(rng, B, top, E)
+    check_layer(mq, x, host, dev, ids, weight, 192, 64, r, True, True)
+
+
+def test_layer_of_large_numbers(mq):
+    """Gated products around 2^40, of both signs, and around 2^-40: two bf16 parts keep 16 bits of either."""
+    rng = np.random.default_rng(25)
+    host, dev = make_layer(rng, 3, 64, 96, 32, 4)
+    x, (ids, weight) = bf16(rng.standard_normal((4, 64))), choices(rng, 4, 2, 3)
+    x[:2] *= 2.0 ** 20
+    x[2:] *= 2.0 ** -20
+    check_layer(mq, x, host, dev, ids, weight, 96, 32, 4, True, False)
+
+
 def test_layer_token_of_no_numbers_is_alone(mq):
     """A token of NaN beside others that share its experts; a weight of NaN likewise."""
     rng = np.random.default_rng(22)
