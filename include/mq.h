@@ -572,8 +572,9 @@ mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place, const floa
  *   alpha_bf16, zero_bf16  [N, K / group] bf16
  *   y       [B, N] bf16 out; may not overlap an input
  * group a multiple of 32 (r = 2: of 64; MQ_ERR_ALIGN) that divides K; K itself is one pair per row.  K <= 2^20, N <= 2^25 (MQ_ERR_SHAPE
- * beyond).  N == 0 is a no-op.  A token that holds an infinity or a NaN has outputs that are no numbers, and one whose |x| add up to 2^120 or
- * more inside a group may have (sums overflow); no other token's are touched.  The order of the fp32 sums is fixed by B, N, K, group and r.
+ * beyond).  N == 0 is a no-op.  A token that holds an infinity or a NaN has outputs that are no numbers.  One may have (sums overflow) whose
+ * |x| times 2^8 + |z| / 2^(8-r) add up to 2^127 or more inside a group, or whose |w x|, w = alpha (2^(8-r) code - z), do over a row.  No
+ * other token's outputs are touched.  The order of the fp32 sums is fixed by B, N, K, group and r.
  */
 mq_status mq_gemv_grouped(const uint16_t *x, const uint8_t *packed, const uint16_t *alpha_bf16, const uint16_t *zero_bf16,
                           int64_t B, int64_t N, int64_t K, int64_t group, int r, uint16_t *y, void *hip_stream);
@@ -607,8 +608,8 @@ mq_status mq_experts_choose_bwd(const float *scores, int64_t ld, const int32_t *
  * A whole feed-forward layer of experts for up to 16 tokens in two launches, on planes with group scales (mq_experts_route and
  * mq_experts_fwd_int8 are the way for more):
  *     y_b = sum_j weight[b,j] * W_down[e] (act(W_gate[e] x_b) * W_up[e] x_b)        e = ids[b,j]
- * (+ x_b with MQ_FLAG_FFN_RESIDUAL).  Products as mq_gemv_grouped forms them; fp32 up to y, only the gated products are held in 16
- * significant bits in between.  A chosen expert's gate / up rows are read once, its down plane once for every 8
+ * (+ x_b with MQ_FLAG_FFN_RESIDUAL).  Products as mq_gemv_grouped forms them, its limits on large numbers for the gated products too; fp32 up
+ * to y, only the gated products are held in 16 significant bits in between.  A chosen expert's gate / up rows are read once, its down plane once for every 8
  * of its tokens, planes of experts that nobody chose not at all.
  *   x        [B, d] bf16, 1 <= B <= 16
  *   layer    HOST descriptor as for mq_ffn_mixnmatch, its arrays those of all experts, one after the other: gate_up [E, 2F, d*r/8] (row

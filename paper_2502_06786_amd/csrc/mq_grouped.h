@@ -9,7 +9,8 @@ namespace mq {
 // y[t, n] = sum over groups of alpha (2^s sum code x - z sum x).  A wave takes tiles of 16 rows of the plane (the matrix core's columns: lane
 // & 15) and up to 16 tokens (its rows), 32 codes to a step.  Two products run side by side: tokens x codes and tokens x ones, whose result is
 // sum x in the very lanes that hold the tokens' products; both are whole sums in fp32 over a chunk (a part of one group) before they meet
-// alpha and z.  Codes of 4 bits enter as 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of them), which
+// z, and alpha meets their difference, the codes' offset gone: large sums that take each other out do so before they are scaled, with one
+// rounding of what is left.  Codes of 4 bits enter as 128 + code (a bf16 number that holds the code exactly: shift, mask and or for two of them), which
 // sum x takes out again.  Two bits at mantissa bits 0, 2 or 4 under the exponent of 128, 32 or 8 are such numbers too, so codes of 2 bits need two
 // shifts to a register instead of seven; a third product, of the tokens with the negative of these, stands in the sums before the codes do.
 //
@@ -120,7 +121,8 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
     // code pair j of a register of 2-bit codes stands at position j % 3 after a shift by 6 (j / 3)
     const u32x4 minus[2] = {{0xC300C300u, 0xC200C200u, 0xC100C100u, 0xC300C300u}, {0xC200C200u, 0xC100C100u, 0xC300C300u, 0xC200C200u}};
     uint8_t *const lds_x = lds + G::CODES;
-    f32pair_t *const lds_params = reinterpret_cast<f32pair_t *>(lds_x + G::TOKENS);  // what a chunk's two sums are multiplied with
+    // alpha 2^s, what sum x is multiplied with before it
+    f32pair_t *const lds_params = reinterpret_cast<f32pair_t *>(lds_x + G::TOKENS);
 
     uint32_t row_codes[RG][2], row_params[RG];
 #pragma unroll
@@ -234,7 +236,7 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
             for (int t = 0; t < RG; ++t) {
                 const f32pair_t by = lds_params[(t * 4 * NC + chunk) * 16 + li];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[t][i] = __builtin_fmaf(by[0], dot[t][i], __builtin_fmaf(by[1], sum[i], y[t][i]));
+                for (int i = 0; i < 4; ++i) y[t][i] = __builtin_fmaf(by[0], __builtin_fmaf(by[1], sum[i], dot[t][i]), y[t][i]);
                 asm volatile("" : "+v"(y[t]));  // (done here: put off to where y is used, every chunk's sums would stay in registers)
             }
         }
@@ -256,7 +258,7 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
             for (int i = 0; i < NC; ++i) {
                 const float a = s.first * NC + 4 * i + part < chunks ? bf16_bits_to_float(alpha[t][i]) : 0.f;
                 lds_params[(t * 4 * NC + 4 * i + part) * 16 + (lane >> 2)] =
-                    f32pair_t{a * step, -a * __builtin_fmaf(step, kCodeOffset<R>, bf16_bits_to_float(zero[t][i]))};
+                    f32pair_t{a * step, -__builtin_fmaf(1.0f / step, bf16_bits_to_float(zero[t][i]), kCodeOffset<R>)};
             }
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {

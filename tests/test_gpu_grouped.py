@@ -98,6 +98,23 @@ def test_gemv_token_of_no_numbers_is_alone(mq):
         assert not torch.isfinite(got[[5, 15]]).any()
 
 
+@pytest.mark.parametrize("B", [1, 6, 16])
+@pytest.mark.parametrize("r,group", [(4, 32), (4, 64), (4, 128), (2, 64), (2, 128), (2, 256), (8, 32), (8, 64)])
+def test_gemv_of_weights_that_are_zero_under_large_tokens(mq, B, r, group):
+    """Large |x| meet only weights that are 0 (code = z), under a scale of 2^9: what is exactly 0 inside a group stays 0.  Sum of |x| 2^118 in a group."""
+    rng = np.random.default_rng(r * group + B)
+    N, K, code = 35, 5 * group, {8: 130, 4: 9, 2: 3}[r]
+    codes = np.full((N, K), code)
+    alpha, zero = np.full((N, 5), 512.0), np.full((N, 5), code * 2.0 ** (8 - r))
+    x = np.zeros((B, K))
+    for g in range(5):
+        at = g * group + rng.choice(group, 16, replace=False)
+        x[:, at] = 2.0 ** 114
+        other = np.setdiff1d(np.arange(g * group, (g + 1) * group), at)
+        codes[:, other] = rng.integers(0, 1 << r, (N, len(other)))
+    assert not gemv(mq, x, codes, alpha, zero, r, group).float().any()
+
+
 def test_gemv_of_what_the_library_quantizes(mq):
     """Groups are rows of a view: quantize, slice, round, multiply."""
     rng = np.random.default_rng(5)
