@@ -573,8 +573,8 @@ mq_status mq_experts_combine(const uint16_t *Y, const int32_t *place, const floa
  *   y       [B, N] bf16 out; may not overlap an input
  * group a multiple of 32 (r = 2: of 64; MQ_ERR_ALIGN) that divides K; K itself is one pair per row.  K <= 2^20, N <= 2^25 (MQ_ERR_SHAPE
  * beyond).  N == 0 is a no-op.  A token that holds an infinity or a NaN has outputs that are no numbers.  One may have (sums overflow) whose
- * |x| times 2^8 + |z| / 2^(8-r) add up to 2^127 or more inside a group, or whose |w x|, w = alpha (2^(8-r) code - z), do over a row.  No
- * other token's outputs are touched.  The order of the fp32 sums is fixed by B, N, K, group and r.
+ * |x| times 2^8 + |z| / 2^(8-r) add up to 2^127 or more inside a group, or whose |w x|, w = alpha (2^(8-r) code - z), do over a row
+ * (alpha 2^(8-r) below 2^127 too).  No other token's outputs are touched.  The order of the fp32 sums is fixed by B, N, K, group and r.
  */
 mq_status mq_gemv_grouped(const uint16_t *x, const uint8_t *packed, const uint16_t *alpha_bf16, const uint16_t *zero_bf16,
                           int64_t B, int64_t N, int64_t K, int64_t group, int r, uint16_t *y, void *hip_stream);

@@ -112,15 +112,14 @@ __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(Expe
         int at = wave;
         uint32_t begin[G::XI];
 #pragma unroll
-        for (int i = 0; i < G::XI; ++i) begin[i] = 2 * (uint32_t)(take_from(min(load_token<G>(i), count - 1), token) * a.d);
+        for (int i = 0; i < G::XI; ++i) begin[i] = 2 * (uint32_t)(take_from(min(load_token<G>(i), count - 1), token) * a.d + load_input<G>(i));
         grouped_stream<R, C, RG, T, false, decltype(ahead)::value>(
-            lds + wave * Grouped<R, C, RG, MOST>::LDS, 2 * a.F - row0, a.d, a.groups_d, a.group, y,
+            lds + wave * Grouped<R, C, RG, MOST>::LDS, token_buffer(a.x, 2 * (uint32_t)(a.B * a.d)), 2 * a.F - row0, a.d, a.groups_d, a.group, y,
             [&](Stretch<G::XI> &s) {
                 if (at >= stretches) return false;
                 s.codes = a.gate_up + first_row * (a.d / 8 * R);
                 s.alpha = a.alpha_gu + first_row * a.groups_d;
                 s.zero = a.zero_gu + first_row * a.groups_d;
-                s.x = a.x;
 #pragma unroll
                 for (int i = 0; i < G::XI; ++i) s.token[i] = begin[i];
                 s.first = at * kPieces * kHalves;
@@ -202,7 +201,7 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
         using G = Grouped<R, C, RG, 2 * TOKENS>;
         int item = start;
         grouped_stream<R, C, RG, 2 * TOKENS, true, decltype(ahead)::value>(
-            mine, a.d - row0, a.F, a.groups_F, a.group, y,
+            mine, token_buffer(a.act, 2 * (rest + (uint32_t)(a.n * a.F))), a.d - row0, a.F, a.groups_F, a.group, y,
             [&](Stretch<G::XI> &s) {
                 if (item >= items) return false;
                 const int which = item / stretches;
@@ -213,11 +212,10 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
                 s.codes = a.down + first_row * (a.F / 8 * R);
                 s.alpha = a.alpha_dn + first_row * a.groups_F;
                 s.zero = a.zero_dn + first_row * a.groups_F;
-                s.x = a.act;
 #pragma unroll
                 for (int i = 0; i < G::XI; ++i) {
                     const int t = load_token<G>(i) % (2 * TOKENS);
-                    s.token[i] = 2 * ((uint32_t)a.row[entry * 8 + min(t % TOKENS, s.count - 1)] * (uint32_t)a.F + (t < TOKENS ? 0u : rest));
+                    s.token[i] = 2 * ((uint32_t)a.row[entry * 8 + min(t % TOKENS, s.count - 1)] * (uint32_t)a.F + (t < TOKENS ? 0u : rest) + load_input<G>(i));
                 }
                 s.first = (item - which * stretches) * kPieces * kHalves;
                 s.tokens = *reinterpret_cast<const uint32_t *>(a.token + entry * 8 + 4 * (quarter & 1));

@@ -83,8 +83,7 @@ template <int XI>
 struct Stretch {
     const uint8_t *codes;          // row 0 of the tiles, code 0 of the rows
     const uint16_t *alpha, *zero;  // row 0 of the tiles, group 0
-    const uint16_t *x;
-    uint32_t token[XI];            // begin of the token that a lane loads for (bytes, from x)
+    uint32_t token[XI];            // the first input that a lane loads of its token, as if half piece 0 came first (bytes, from the first token)
     int first;                     // first half piece
     // the layer's down product: whose outputs a lane's y are
     int count;                     // tokens
@@ -94,18 +93,30 @@ struct Stretch {
 // Between what lanes of a wave leave in LDS and what others of it read there: LDS serves a wave in order, so the compiler alone has to keep it.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// Which token a lane's i-th load of half a piece is for.
+// Which token a lane's i-th load of half a piece is for, and which of the half piece's inputs is the first that it brings.
 template <typename G>
 __device__ __forceinline__ int load_token(int i) {
     return (64 * i + (int)(threadIdx.x & 63)) / G::XS;
+}
+template <typename G>
+__device__ __forceinline__ int load_input(int i) {
+    return (64 * i + (int)(threadIdx.x & 63)) % G::XS * 8;
+}
+
+// `bytes` bytes of tokens (less than 2^31) from x: a load behind them gives zeros.
+constexpr uint32_t kBehind = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t token_buffer(const uint16_t *x, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x), 0, (int)bytes, 0x00020000);  // (no stride, data of 32 bits)
 }
 
 // Does stretch after stretch: next(s) gives the wave's next one or says that there is none, end(s, more) follows each (with more, next has
 // been asked for the one behind it already); products are added to y[tile] (lane & 15 = row, component i = token 4 (lane >> 4) + i).  While a piece is
 // multiplied the D - 1 behind it are on their way; nothing is requested behind the last stretch.  ORDERED: tokens are in operand order.
-// What lies behind the end of rows of K inputs is read as their end again and counts for nothing.
+// What lies behind the end of rows of K inputs is read as their end again, but for tokens, which are zeros there (a scale of zero alone would make
+// no number of sums that overflow there alone): the places are out of the buffer's range, so the load gives zeros without a branch or a select of
+// what it brings.
 template <int R, int C, int RG, int T, bool ORDERED, int D, typename Next, typename End>
-__device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, int groups, GroupOf group, f32x4 (&y)[RG], Next next, End end) {
+__device__ __forceinline__ void grouped_stream(uint8_t *lds, __amdgpu_buffer_rsrc_t tokens, int rows, int K, int groups, GroupOf group, f32x4 (&y)[RG], Next next, End end) {
     using G = Grouped<R, C, RG, T>;
     constexpr int PC = G::PC, NC = G::NC, STEPS = G::STEPS, XS = G::XS, XI = G::XI;
     static_assert((D == 1 || D == 2) && NC >= 1 && STEPS >= 1 && (R != 2 || STEPS % 2 == 0), "");
@@ -154,8 +165,9 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
         for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int i = 0; i < XI; ++i) {
-                const uint32_t v = s.token[i] + 2 * (uint32_t)min((s.first + kHalves * j + h) * PC + (64 * i + lane) % XS * 8, K - 8);
-                x[slot][h][i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(s.x) + v);
+                const int begin = (s.first + kHalves * j + h) * PC;
+                const uint32_t v = load_input<G>(i) < K - begin ? s.token[i] : kBehind;
+                x[slot][h][i] = __builtin_amdgcn_raw_buffer_load_b128(tokens, (int)v, 2 * begin, 0);
             }
     };
     auto fetch_params = [&](const Stretch<XI> &s) {
@@ -256,7 +268,7 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, int rows, int K, in
         for (int t = 0; t < RG; ++t)
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const float a = s.first * NC + 4 * i + part < chunks ? bf16_bits_to_float(alpha[t][i]) : 0.f;
+                const float a = bf16_bits_to_float(alpha[t][i]);
                 lds_params[(t * 4 * NC + 4 * i + part) * 16 + (lane >> 2)] =
                     f32pair_t{a * step, -__builtin_fmaf(1.0f / step, bf16_bits_to_float(zero[t][i]), kCodeOffset<R>)};
             }

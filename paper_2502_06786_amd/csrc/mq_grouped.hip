@@ -34,15 +34,14 @@ __global__ __launch_bounds__(64 * gemv_waves(R, C, RG, T, D)) void gemv_grouped_
     for (int t = 0; t < RG; ++t) y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     int at = wave;
     grouped_stream<R, C, RG, T, false, D>(
-        lds + wave * G::LDS, a.N - row0, a.K, a.groups, a.group, y,
+        lds + wave * G::LDS, token_buffer(a.x, 2 * (uint32_t)(a.B * a.K)), a.N - row0, a.K, a.groups, a.group, y,
         [&](Stretch<G::XI> &s) {
             if (at >= stretches) return false;
             s.codes = a.packed + (int64_t)row0 * (a.K / 8 * R);
             s.alpha = a.alpha + (int64_t)row0 * a.groups;
             s.zero = a.zero + (int64_t)row0 * a.groups;
-            s.x = a.x;
 #pragma unroll
-            for (int i = 0; i < G::XI; ++i) s.token[i] = 2 * (uint32_t)(min(load_token<G>(i), a.B - 1) * a.K);
+            for (int i = 0; i < G::XI; ++i) s.token[i] = 2 * (uint32_t)(min(load_token<G>(i), a.B - 1) * a.K + load_input<G>(i));
             s.first = at * kPieces * kHalves;
             at += a.ks;
             return true;

@@ -115,6 +115,22 @@ def test_gemv_of_weights_that_are_zero_under_large_tokens(mq, B, r, group):
     assert not gemv(mq, x, codes, alpha, zero, r, group).float().any()
 
 
+# rows that end inside a half piece: what stands behind their end there is chunks of 32 to 128 codes
+@pytest.mark.parametrize("B", [1, 6, 16])
+@pytest.mark.parametrize("r,K,group", [(4, 32, 32), (4, 64, 64), (4, 64, 32), (4, 160, 32), (4, 576, 192), (2, 64, 64), (2, 128, 128), (2, 1152, 384), (8, 32, 32), (8, 288, 96)])
+def test_gemv_of_a_large_last_input(mq, B, r, K, group):
+    """A row's last input is 0.94 2^119, under a scale of 2^-118 and a zero-point of 0: the sums are below their limit if the end of the row counts once."""
+    rng = np.random.default_rng(K + B)
+    codes, alpha, zero = whole_plane(rng, 19, K, group, r)
+    codes[:, -1], alpha[:, -1], zero[:, -1] = (1 << r) - 1, 2.0 ** -118, 0.0
+    x = rng.integers(-2, 3, (B, K)).astype(np.float64)
+    x[:, -group:] = 0.0
+    x[:, -1] = 1.875 * 2.0 ** 118
+    y, bar = ref.product(x, codes, alpha, zero, r)
+    got = gemv(mq, x, codes, alpha, zero, r, group).cpu().double().numpy()
+    assert (np.abs(got - y) <= bar + ref.BF16 * (np.abs(y) + bar)).all()
+
+
 def test_gemv_of_what_the_library_quantizes(mq):
     """Groups are rows of a view: quantize, slice, round, multiply."""
     rng = np.random.default_rng(5)
@@ -311,6 +327,27 @@ def test_layer_of_large_numbers(mq):
     x[:2] *= 2.0 ** 20
     x[2:] *= 2.0 ** -20
     check_layer(mq, x, host, dev, ids, weight, 96, 32, 4, True, False)
+
+
+@pytest.mark.parametrize("r,F,group", [(4, 32, 32), (4, 128, 128), (4, 160, 32), (4, 640, 128), (2, 256, 256), (8, 64, 64), (8, 96, 32)])
+def test_layer_of_large_last_gated_products(mq, r, F, group):
+    """Every expert's last eight gated products add up to 0.92 2^119, under scales of 2^-116 and zero-points of 0; more experts than the down product has
+    waves, so a wave that is through with one goes on to another: what it reads behind a row's end counts for nothing."""
+    rng = np.random.default_rng(F + r)
+    B, top, E, d = 16, 16, 120, max(group, 64)
+    host, dev = make_layer(rng, E, d, F, group, r)
+    code, step = (1 << r) - 1, 2.0 ** (8 - r)
+    host["codes_gu"][:], host["zero_gu"][:] = code, code * step
+    host["codes_gu"][:, -16:, 0] = code - 1                      # the last eight pairs of rows alone have a weight that is not 0, their first one
+    host["alpha_gu"][:, 0::2], host["alpha_gu"][:, 1::2] = -2.0 ** 57 / step, -2.0 ** 58 / step
+    host["codes_dn"][:, :, -8:], host["alpha_dn"][:], host["zero_dn"][:] = code, 2.0 ** -116, 0.0
+    for name, short in (("gate_up", "gu"), ("down", "dn")):
+        dev[name] = to_gpu(ref.pack(host["codes_" + short], r))
+        dev["zero_" + short], dev["alpha_" + short] = to_gpu(host["zero_" + short], torch.bfloat16), to_gpu(host["alpha_" + short], torch.bfloat16)
+    x = np.zeros((B, d))
+    x[:, 0] = 1.359375   # gated products: 2^57 x 2^58 x, eight of them 2^118.89
+    ids, weight = choices(rng, B, top, E)
+    check_layer(mq, x, host, dev, ids, weight, F, group, r, True, False)
 
 
 def test_layer_token_of_no_numbers_is_alone(mq):
