@@ -167,7 +167,8 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, __amdgpu_buffer_rsr
             for (int i = 0; i < XI; ++i) {
                 const int begin = (s.first + kHalves * j + h) * PC;
                 const uint32_t v = load_input<G>(i) < K - begin ? s.token[i] : kBehind;
-                x[slot][h][i] = __builtin_amdgcn_raw_buffer_load_b128(tokens, (int)v, 2 * begin, 0);
+                // (a scalar offset inside the buffer: the range that is left for v is the buffer's less this one)
+                x[slot][h][i] = __builtin_amdgcn_raw_buffer_load_b128(tokens, (int)v, 2 * min(begin, K - 8), 0);
             }
     };
     auto fetch_params = [&](const Stretch<XI> &s) {
