@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(Expe
         }
     }
 
-    const int row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.d + kStretchCodes<R> - 1) / kStretchCodes<R>;
+    const int row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.d + stretch_codes(R) - 1) / stretch_codes(R);
     const int64_t first_row = (int64_t)e * 2 * a.F + row0;
     f32x4 y[RG];
 #pragma unroll
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     using Lds = DownLds<R, C, RG, MOST>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
-    const int waves = (int)(blockDim.x >> 6), row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.F + kStretchCodes<R> - 1) / kStretchCodes<R>;
+    const int waves = (int)(blockDim.x >> 6), row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.F + stretch_codes(R) - 1) / stretch_codes(R);
     uint8_t *const mine = lds + Lds::LIST + wave * Lds::WAVE;
     float *const sums = reinterpret_cast<float *>(mine + Lds::STREAM);  // [token][row]
     // (entry, tokens << 16; expert): entries of up to 4 tokens from the front, of more from the back
@@ -278,8 +278,6 @@ struct ExpertsFfnLayout {
     size_t act, rest, count, expert, token, row, share, part, arrived, total;
 };
 
-constexpr int kDownSplits = 8;  // workgroups that share rows, at most
-
 ExpertsFfnLayout experts_ffn_layout(int64_t n, int64_t F, int64_t d) {
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
     ExpertsFfnLayout l;
@@ -299,7 +297,7 @@ ExpertsFfnLayout experts_ffn_layout(int64_t n, int64_t F, int64_t d) {
 template <int R, int C, int RG, int MOST, int D>
 mq_status launch_gate_up_as(ExpertsFfnArgs a, hipStream_t st) {
     constexpr int LDS = Grouped<R, C, RG, MOST>::LDS;
-    const int64_t stretches = cdiv(a.d, kStretchCodes<R>), blocks = cdiv(2 * a.F, kGroupedRows * RG);
+    const int64_t stretches = cdiv(a.d, stretch_codes(R)), blocks = cdiv(2 * a.F, kGroupedRows * RG);
     // (waves as for the product alone: 24 for each compute unit)
     a.ks = (int)std::min<int64_t>({stretches, kGateUpWaves, 163840 / LDS, cdiv(24 * 256, blocks * std::min(a.n, a.E))});
     a.ks = (int)cdiv(stretches, cdiv(stretches, a.ks));
@@ -312,10 +310,8 @@ mq_status launch_gate_up_as(ExpertsFfnArgs a, hipStream_t st) {
 template <int R, int C, int RG, int MOST, int D>
 mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
     using Lds = DownLds<R, C, RG, MOST>;
-    const int64_t items = cdiv(a.F, kStretchCodes<R>) * std::min(a.n, a.E), blocks = cdiv(a.d, kGroupedRows * RG);
-    // a workgroup for each compute unit, of as many waves as there are items and room (16 tokens x 4 of 128, 2048 x 1408: 50 us, with workgroups
-    // of their own rows only 78; x 2 of 8, 4096 x 14336: 168 and 209; one token x 8 of 64, 2048 x 1024: 14.0 both)
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kDownSplits, 256 / blocks, items / 8}));
+    const int64_t items = cdiv(a.F, stretch_codes(R)) * std::min(a.n, a.E), blocks = cdiv(a.d, kGroupedRows * RG);
+    a.splits = down_splits(R, a.d, a.F, std::min(a.n, a.E), RG);
     const int waves = (int)std::min<int64_t>({cdiv(items, a.splits), down_waves(R), (163840 - Lds::LIST) / Lds::WAVE});
     const int lds = Lds::LIST + waves * Lds::WAVE;
     constexpr auto kernel = experts_down_kernel<R, C, RG, MOST, D>;
@@ -325,21 +321,18 @@ mq_status launch_down_as(ExpertsFfnArgs a, hipStream_t st) {
 }
 template <int R, int C, int MOST>
 mq_status launch_gate_up(const ExpertsFfnArgs &a, hipStream_t st) {
-    // Two tiles to a wave, which share the tokens' way through LDS, where that leaves enough waves (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us,
-    // with one 180; 2 tokens x 4 of 64, 2048 x 768: 13.2 with one, 14.5 with two); a piece under way beside the one that is
-    // multiplied (one token x 2 of 8, 4096 x 14336: 47.2 us, without 49.7), but at two bits, which want registers for more waves (5 tokens x 2 of 8,
-    // 2304 x 9216: 55.0, with it 58.3).
+    // A piece under way beside the one that is multiplied (one token x 2 of 8, 4096 x 14336: 47.2 us, without 49.7), but at two bits, which want
+    // registers for more waves (5 tokens x 2 of 8, 2304 x 9216: 55.0, with it 58.3).
     constexpr int D = R == 2 ? 1 : 2;
-    if (cdiv(2 * a.F, 2 * kGroupedRows) * std::min(a.n, a.E) >= 2048) return launch_gate_up_as<R, C, 2, MOST, D>(a, st);
+    if (gate_up_tiles(a.F, std::min(a.n, a.E)) == 2) return launch_gate_up_as<R, C, 2, MOST, D>(a, st);
     return launch_gate_up_as<R, C, 1, MOST, D>(a, st);
 }
 template <int R, int C, int MOST>
 mq_status launch_down(const ExpertsFfnArgs &a, hipStream_t st) {
-    // Tiles as above (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us, with one 181; one token x 8 of 64, 2048 x 1024: 14.1 with one, 15.7 with two).
     // A piece under way helps small layers (2 tokens x 4 of 64, 2048 x 768: 13.2 us, without 14.0), at two bits it makes no odds (16 tokens x 2 of 8,
     // 4096 x 14336: 155.8, without 153.9; 5 tokens x 2 of 8, 2304 x 9216: 53.6 and 55.2), groups of 32 at four bits leave no registers for it.
     constexpr int D = R == 2 || (R == 4 && C == 32) ? 1 : 2;
-    if (cdiv(a.d, 2 * kGroupedRows) * std::min(a.n, a.E) * cdiv(a.F, kStretchCodes<R>) >= 2048) return launch_down_as<R, C, 2, MOST, D>(a, st);
+    if (down_tiles(R, a.d, a.F, std::min(a.n, a.E)) == 2) return launch_down_as<R, C, 2, MOST, D>(a, st);
     return launch_down_as<R, C, 1, MOST, D>(a, st);
 }
 template <int R, int C>

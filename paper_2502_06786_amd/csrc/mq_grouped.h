@@ -3,6 +3,7 @@
 #pragma once
 
 #include "mq_common.h"
+#include "mq_grouped_plan.h"
 
 namespace mq {
 
@@ -20,7 +21,6 @@ namespace mq {
 //
 // In operand order a register holds codes j and j + 4 (r = 4; j and j + 8 for r = 2) of a lane's run of 8 (16), since that is what one shift and
 // mask leaves.
-constexpr int kGroupedTokens = 16, kGroupedRows = 16;
 
 // what sum x takes out of the products
 template <int R>
@@ -43,15 +43,6 @@ inline GroupOf group_of(int64_t cpg) {
     return cpg == 1 ? GroupOf{0u, ~0u} : GroupOf{(uint32_t)(((1ull << 32) + cpg - 1) / cpg), 0u};
 }
 
-// inputs of a group have to be whole steps of the matrix core and whole pieces of 16 bytes
-inline int64_t group_unit(int r) { return r == 2 ? 64 : 32; }
-// codes of a chunk: those of a piece, or as far as groups allow it
-inline int chunk_codes(int r, int64_t group) {
-    int c = 512 / r;
-    while (group % c != 0) c >>= 1;
-    return c;
-}
-
 __device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
@@ -62,11 +53,8 @@ __device__ __forceinline__ f32x4 mfma_tokens(u32x4 tokens, u32x4 codes, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
 }
 
-constexpr int kHalves = 2, kPieces = 2;  // 64-byte halves of a piece, pieces of a stretch
 template <int R>
 constexpr int kHalfCodes = 512 / R;
-template <int R>
-constexpr int kStretchCodes = kPieces * kHalves * kHalfCodes<R>;
 
 // T: tokens that are loaded, 4, 8 or 16 (the rows of the matrix core behind them repeat them); C codes to a chunk; RG tiles of 16 rows.
 template <int R, int C, int RG, int T>

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(64 * gemv_waves(R, C, RG, T, D)) void gemv_grouped_
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     using G = Grouped<R, C, RG, T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, quarter = lane >> 4;
-    const int row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.K + kStretchCodes<R> - 1) / kStretchCodes<R>;
+    const int row0 = (int)blockIdx.x * kGroupedRows * RG, stretches = (a.K + stretch_codes(R) - 1) / stretch_codes(R);
     f32x4 y[RG];
 #pragma unroll
     for (int t = 0; t < RG; ++t) y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -72,7 +72,7 @@ mq_status grouped_check(const uint8_t *packed, const uint16_t *alpha, const uint
 template <int R, int C, int RG, int T, int D>
 static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
     using G = Grouped<R, C, RG, T>;
-    const int64_t stretches = cdiv(a.K, kStretchCodes<R>), blocks = cdiv(a.N, kGroupedRows * RG);
+    const int64_t stretches = cdiv(a.K, stretch_codes(R)), blocks = cdiv(a.N, kGroupedRows * RG);
     // Waves of a workgroup: 12 on each compute unit where there is no more than a workgroup or two for each (4096 x 14336, B = 16: 11.8 us, with
     // 14 waves instead of 10 12.9), otherwise 24, of which 16 to 20 are there at a time (73728 x 4608, B = 1: 34.9 us, half as many 39.4).
     const int64_t wanted = cdiv((blocks <= 512 ? 12 : 24) * 256, blocks);
@@ -85,19 +85,13 @@ static mq_status launch_gemv_grouped_as(GroupedGemvArgs a, hipStream_t st) {
     return launch_status();
 }
 
-// Tiles of a wave and pieces under way.  Two tiles share the tokens' way through LDS, which counts for 16 tokens from 8192 rows on (14336 x
-// 4096, B = 16: 10.2 us with two, 12.3 with one; 4096 x 14336: 14.4 and 11.8), for up to 4 where memory is kept busy by half as many
-// waves (73728 x 4608, B = 1, r = 4: 34.9 and 37.0 us; 28672 x 4096: 13.5 and 13.0), at two bits, which are bound by the vector unit, earlier
-// (28672 x 4096: 12.9 and 13.5).  Groups of 32 at four bits leave no registers for it (73728 x 4608: 57 and 51 us).
-template <int R, int C>
+template <int R, int C, int T>
 static mq_status launch_gemv_grouped(const GroupedGemvArgs &a, hipStream_t st) {
-    if (a.B > 8) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 16, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 16, 1>(a, st);
-    if (a.B > 4) return a.N >= 8192 ? launch_gemv_grouped_as<R, C, 2, 8, 1>(a, st) : launch_gemv_grouped_as<R, C, 1, 8, 1>(a, st);
-    if constexpr (R == 4 && C == 32) return launch_gemv_grouped_as<R, C, 1, 4, 2>(a, st);
-    if constexpr (R != 4 || C != 32) {
-        if (a.N >= (R == 4 ? 65536 : 16384)) return launch_gemv_grouped_as<R, C, 2, 4, 2>(a, st);
-        return launch_gemv_grouped_as<R, C, 1, 4, R == 2 ? 1 : 2>(a, st);
-    }
+    // (a piece under way beside the one that is multiplied, where registers allow it)
+    constexpr int D1 = T > 4 || R == 2 ? 1 : 2, D2 = T > 4 ? 1 : 2;
+    if constexpr (gemv_two_tiles_fit(R, C, T))
+        if (gemv_tiles(R, C, a.B, a.N) == 2) return launch_gemv_grouped_as<R, C, 2, T, D2>(a, st);
+    return launch_gemv_grouped_as<R, C, 1, T, D1>(a, st);
 }
 
 }  // namespace mq
@@ -113,8 +107,11 @@ extern "C" mq_status mq_gemv_grouped(const uint16_t *x, const uint8_t *packed, c
     const int c = chunk_codes(r, group);
     const GroupedGemvArgs a{x, packed, alpha_bf16, zero_bf16, y, (int)B, (int)N, (int)K, (int)(K / group), 1, group_of(group / c)};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-#define MQ_GROUPED_CASE(R_, C_) \
-    if (r == R_ && c == C_) return launch_gemv_grouped<R_, C_>(a, st);
+#define MQ_GROUPED_CASE(R_, C_)                                                    \
+    if (r == R_ && c == C_)                                                        \
+        return token_class(B) == 4   ? launch_gemv_grouped<R_, C_, 4>(a, st)       \
+               : token_class(B) == 8 ? launch_gemv_grouped<R_, C_, 8>(a, st)       \
+                                     : launch_gemv_grouped<R_, C_, 16>(a, st);
     MQ_GROUPED_CASE(4, 128) MQ_GROUPED_CASE(4, 64) MQ_GROUPED_CASE(4, 32)
     MQ_GROUPED_CASE(2, 256) MQ_GROUPED_CASE(2, 128) MQ_GROUPED_CASE(2, 64)
     MQ_GROUPED_CASE(8, 64) MQ_GROUPED_CASE(8, 32)

@@ -11,7 +11,7 @@
 
 namespace mq {
 
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 constexpr int BKT = 64;                  // contraction elements per LDS stage

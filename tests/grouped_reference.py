@@ -1,6 +1,7 @@
 """Products with group scales, the choice of experts and the layer of experts for a few tokens from their definitions in 64 bits, and how
 far a correct implementation may be off."""
 import numpy as np
+import torch
 
 U32 = 2.0 ** -24   # half a step of fp32, relative
 BF16 = 2.0 ** -8   # half a step of bf16, relative
@@ -66,6 +67,41 @@ def layer(x, L, ids, weight, r, silu, residual=False):
     if residual:
         y = y + x
     return y, bar + BF16 * (np.abs(y) + bar)
+
+
+def product_on(x, packed, alpha, zero, r):
+    """`product` on tensors of any device, codes packed."""
+    x, alpha, zero = x.double(), alpha.double(), zero.double()
+    rows, groups = alpha.shape
+    group, step, offset = x.shape[1] // groups, 2.0 ** (8 - r), 0.0 if r == 8 else 128.0
+    codes = torch.stack([(packed >> (r * i)) & ((1 << r) - 1) for i in range(8 // r)], -1).view(rows, groups, group)
+    w = alpha[..., None] * (step * codes.double() - zero[..., None])
+    size = alpha.abs()[..., None] * (step * (codes.double() + offset) + zero.abs()[..., None] + step * offset)
+    chunk = min(group, 512 // r)
+    return x @ w.view(rows, -1).t(), U32 * (chunk + x.shape[1] / chunk + 32) * (x.abs() @ size.view(rows, -1).t())
+
+
+def layer_on(x, L, ids, weight, r, silu, residual=False):
+    """`layer` on tensors of any device: packed_gu [E, 2F, d r / 8] and so on; an expert with all its tokens at a time."""
+    x, weight = x.double(), weight.double()
+    y, bar = torch.zeros_like(x), torch.zeros_like(x)
+    for e in range(L["packed_dn"].shape[0]):
+        token, choice = (ids == e).nonzero(as_tuple=True)
+        if not token.numel():
+            continue
+        h, dh = product_on(x[token], L["packed_gu"][e], L["alpha_gu"][e], L["zero_gu"][e], r)
+        g, u, dg, du = h[:, 0::2], h[:, 1::2], dh[:, 0::2], dh[:, 1::2]
+        act = g * torch.sigmoid(g if silu else 2.0 * (2.0 / np.pi) ** 0.5 * (g + 0.044715 * g ** 3))
+        a, t = act * u, (2.3 * (g + 0.045 * g ** 3)).abs() + 1.0   # (bounds as in `layer`)
+        da = 1.2 * dg * u.abs() + (act.abs() + 1.2 * dg) * du + a.abs() * (2.0 ** -16 + 2.0 ** -20 + 4 * U32 * t)
+        o, do = product_on(a, L["packed_dn"][e], L["alpha_dn"][e], L["zero_dn"][e], r)
+        w = product_on(torch.eye(a.shape[1], dtype=torch.float64, device=x.device), L["packed_dn"][e], L["alpha_dn"][e], L["zero_dn"][e], r)[0]
+        by = weight[token, choice][:, None]
+        y.index_add_(0, token, by * o)
+        bar.index_add_(0, token, by.abs() * (do * 1.01 + da @ w.abs() + 40 * U32 * o.abs()))
+    if residual:
+        y = y + x
+    return y, bar + BF16 * (y.abs() + bar)
 
 
 def choose(scores, top, renormalize):
