@@ -126,7 +126,7 @@ __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(Expe
                 at += a.ks;
                 return true;
             },
-            [](const Stretch<G::XI> &, bool) {});
+            [](const Stretch<G::XI> &) {});
     };
     if (MOST == 4 || count <= 4)
         products(std::integral_constant<int, 4>{}, std::integral_constant<int, D>{});
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(Expert
                 item += step;
                 return true;
             },
-            [&](const Stretch<G::XI> &s, bool) {
+            [&](const Stretch<G::XI> &s) {
 #pragma unroll
                 for (int t = 0; t < RG; ++t) {
 #pragma unroll

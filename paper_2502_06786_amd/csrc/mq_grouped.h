@@ -97,8 +97,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t token_buffer(const uint16_t *x
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x), 0, (int)bytes, 0x00020000);  // (no stride, data of 32 bits)
 }
 
-// Does stretch after stretch: next(s) gives the wave's next one or says that there is none, end(s, more) follows each (with more, next has
-// been asked for the one behind it already); products are added to y[tile] (lane & 15 = row, component i = token 4 (lane >> 4) + i).  While a piece is
+// Does stretch after stretch: next(s) gives the wave's next one or says that there is none, end(s) follows each (next has been asked for the one
+// behind it by then); products are added to y[tile] (lane & 15 = row, component i = token 4 (lane >> 4) + i).  While a piece is
 // multiplied the D - 1 behind it are on their way; nothing is requested behind the last stretch.  ORDERED: tokens are in operand order.
 // What lies behind the end of rows of K inputs is read as their end again, but for tokens, which are zeros there (a scale of zero alone would make
 // no number of sums that overflow there alone): the places are out of the buffer's range, so the load gives zeros without a branch or a select of
@@ -280,11 +280,11 @@ __device__ __forceinline__ void grouped_stream(uint8_t *lds, __amdgpu_buffer_rsr
     };
     while (next(n)) {
         body(std::true_type{});
-        end(s, true);
+        end(s);
         s = n;
     }
     body(std::false_type{});
-    end(s, false);
+    end(s);
 }
 
 // Adds up the tiles of the workgroup's waves (part: one place for each wave and tile) into those of the first one.

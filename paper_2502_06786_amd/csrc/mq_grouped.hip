@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * gemv_waves(R, C, RG, T, D)) void gemv_grouped_
             at += a.ks;
             return true;
         },
-        [](const Stretch<G::XI> &, bool) {});
+        [](const Stretch<G::XI> &) {});
     join_waves<RG>(reinterpret_cast<f32x4 *>(lds), wave, a.ks, y);
     if (wave != 0) return;
 #pragma unroll
