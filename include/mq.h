@@ -605,8 +605,8 @@ mq_status mq_experts_choose_bwd(const float *scores, int64_t ld, const int32_t *
                                 int64_t M, int64_t E, int64_t top, uint32_t flags, float *dscores, void *hip_stream);
 
 /*
- * A whole feed-forward layer of experts for up to 16 tokens in two launches, on planes with group scales.  More tokens take several calls: no
- * other call reads such planes (mq_experts_fwd_int8 takes codes of a byte with one pair per channel).
+ * A whole feed-forward layer of experts for up to 16 tokens in two launches, on planes with group scales.  More tokens take several calls: no call
+ * for more reads planes with group scales (mq_experts_fwd_int8 takes codes of a byte with one pair per channel).
  *     y_b = sum_j weight[b,j] * W_down[e] (act(W_gate[e] x_b) * W_up[e] x_b)        e = ids[b,j]
  * (+ x_b with MQ_FLAG_FFN_RESIDUAL).  Products as mq_gemv_grouped forms them, its limits on large numbers for the gated products too; fp32 up
  * to y, only the gated products are held in 16 significant bits in between.  A chosen expert's gate / up rows are read once, its down plane once for every 8
