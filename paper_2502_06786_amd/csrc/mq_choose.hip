@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
             total += p[v];
         }
         total = token_sum<LPT>(total);
+        // (one quotient for all experts: half a step of fp32 more than a quotient for each, which took 10.5 us instead of 9.6 for 65531 x 64)
         const float scale = total == 0.f ? 0.f : 1.0f / total;
 #pragma unroll
         for (int v = 0; v < V; ++v) p[v] *= scale;
@@ -220,8 +221,12 @@ __global__ __launch_bounds__(256) void choose_bwd_kernel(ChooseBwdArgs a) {
 }
 
 // f(lanes to a token, values to a lane, values to a load) for E experts; vec: rows are whole 16-byte pieces.  The choice takes as many steps
-// between lanes whatever a lane holds, so fewer lanes with more values each are quicker (65531 x 128, 8 of them: 15.9 us with 8 lanes, 17.5 with 16);
-// the gradient, which is bound by memory, wants short loops (65536 x 128: 14.9 us with 16 lanes, 16.8 with 8).
+// between lanes whatever a lane holds, so fewer lanes with more values each are quicker, down to where a wave's registers are full; the gradient, which
+// is bound by memory, wants short loops.  us with half as many lanes, with these, with twice as many, 8 choices out of the softmax over all:
+//   choice     65536 x 64   11.9, 11.6, 25.1    65536 x 128   19.1, 18.1, 24.9    65536 x 256   29.9, 30.7, 45.6
+//   gradient   65536 x 64   10.9, 10.4, 16.4    65536 x 128   17.1, 15.3, 16.5    65536 x 256   28.3, 27.7, 31.2
+// Beyond, 32 lanes instead of 64 would be quicker for the choice: 30000 x 300 27.9 and 33.5, x 512 27.9 and 33.0, 20000 x 1024 34.6 and 37.6 (16 lanes with
+// 32 values: 28.5 and 29.3 for the first two), for the gradient with up to 300 (20.7 and 22.1; x 512 26.4 and 25.6, x 1024 36.2 and 32.3).
 template <bool CHOICE, typename F>
 static void by_experts(int E, bool vec, F f) {
     auto with = [&](auto lanes, auto values) {

@@ -58,9 +58,12 @@ __device__ __forceinline__ int take_from(int from, int v) { return __builtin_amd
 
 // MOST: tokens that an expert may have, 4, 8 or 16.  Experts with up to 4 load no more than 4 (16 tokens x 2 of 8, 4096 x 14336, r = 4: 168 us,
 // otherwise 178; x 4 of 128, 2048 x 1408: 50 and 54.5).
-// At four and eight bits bound by HBM where experts are large (the first of these layers: 499 MB in 99.8 us, 5.0 TB/s), by
-// the start of a workgroup (who chose what, first lines, 2 to 3 us) where they are small (one token x 8 of 64, 2048 x 1024: 18 MB in 7.8 us); at two
-// bits mostly by the vector unit (5 tokens x 2 of 8, 2304 x 9216: 25 to 34 us, 2.4 TB/s; about 45 instructions to 1024 codes and a load, 10 of them unpack).
+// At four and eight bits bound by HBM where experts are large (the first of these layers: 7 or 8 experts, 437 or 499 MB, in 92 to 112 us by card, 4.5 to 5.0 TB/s;
+// at eight bits 0.85 or 0.97 GB in 170 to 200 us, 4.9 to 5.0), by the start of a workgroup (who chose what, first lines, 2 to 3 us) where they are
+// small (one token x 8 of 64, 2048 x 1024: 18 MB in 7.8 us).  At two bits nothing is full (5 tokens x 2 of 8, 2304 x 9216: 26 to 36 us, 2.4 TB/s; vector
+// unit busy for 0.57 of the cycles, matrix core for 0.25, LDS for 0.34; about 45 instructions to 1024 codes and a load, 10 of them unpack; waves wait for
+// memory for 0.42 of their time), and one token takes longer than at four bits (x 2 of 8, 4096 x 14336, groups of 64: 33.5 us, at four bits with groups of 128
+// 28.8; vector unit 0.66).
 template <int R, int C, int RG, int MOST, int D>
 __global__ __launch_bounds__(64 * kGateUpWaves) void experts_gate_up_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -157,9 +160,9 @@ struct DownLds {
 };
 
 // MOST: tokens of an entry, 4 or 8.  blockIdx.y: which of the workgroups that share the rows
-// One workgroup to a compute unit, three waves to a SIMD: bound by waiting (16 tokens x 2 of 8, 4096 x 14336, r = 4: 250 MB in 68 us, 3.7 TB/s, the
-// vector unit busy for 0.39 of the cycles, LDS for 0.37, the matrix core for 0.14), for small layers by start and end (one token x 8 of 64, 2048 x
-// 1024: 9 MB in 6.5 us).
+// One workgroup to a compute unit, three waves to a SIMD: bound by waiting (16 tokens x 2 of 8, 4096 x 14336, r = 4: 250 MB in 62 to 77 us, 3.2 to 3.7 TB/s, 654 MB of
+// requests to the L2, the vector unit busy for 0.46 of the cycles, LDS for 0.46, the matrix core for 0.18, waves waiting for memory for 0.39 of their time;
+// 16 x 4 of 128, 2048 x 1408: 0.34, 0.32, 0.12 and 0.39), for small layers by start and end (one token x 8 of 64, 2048 x 1024: 9 MB in 7.0 us).
 template <int R, int C, int RG, int MOST, int D>
 __global__ __launch_bounds__(64 * down_waves(R)) void experts_down_kernel(ExpertsFfnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];

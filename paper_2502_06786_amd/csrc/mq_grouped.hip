@@ -20,9 +20,12 @@ constexpr int gemv_waves(int R, int C, int RG, int T, int D) {
 }
 
 // A workgroup takes 16 RG rows, its waves stretches of them in turn; the waves' sums meet in LDS.
-// Large planes of four bits are bound by HBM (73728 x 4608, B = 1: 34.7 us, 5.2 TB/s), those of two bits mostly by the vector unit (28672 x 4096, B = 1:
-// 13.6 us, 2.4 TB/s), 16 tokens by vector unit and LDS, which the tokens pass once for every 16 RG rows (4096 x 14336, groups of 32, r = 4: 13.2 us, 2.8
-// TB/s), small planes by launch, first lines and end (4096 x 4096, B = 1: 4.6 us, 1.9 TB/s).
+// Large planes of four and eight bits are bound by HBM (73728 x 4608, r = 4, B = 1: 35.2 us, 5.1 TB/s; 73728 x 4096, r = 8: 63.1 us, 4.9 TB/s; shorter ones are
+// over before that: 28672 x 4096, r = 8: 31.3 us, 4.0 TB/s).  At two bits nothing is full (73728 x 4096, B = 1: 27.5 us, 3.1 TB/s; 28672 x 4096: 13.7 us, 2.7
+// TB/s, with the vector unit busy for 0.53 of the cycles, the matrix core for 0.26, LDS for 0.33; waves wait for memory for 0.27 of their time and for
+// their turn for 0.44).  Nor with 16 tokens, which come from the L2 once for every 16 RG rows (4096 x 14336, groups of 32, r = 4: 13.1 us, 2.8 TB/s, 159 MB of
+// requests to the L2 for a plane of 37 MB; vector unit 0.41, LDS 0.33, matrix core 0.11; waves wait for memory for 0.46 of their time, 2.5 of them to a SIMD).
+// Small planes are bound by launch, first lines and end (4096 x 4096, B = 1: 4.6 us, 1.9 TB/s).
 template <int R, int C, int RG, int T, int D>
 __global__ __launch_bounds__(64 * gemv_waves(R, C, RG, T, D)) void gemv_grouped_kernel(GroupedGemvArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];

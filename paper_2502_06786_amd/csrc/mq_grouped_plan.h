@@ -26,10 +26,19 @@ inline int chunk_codes(int r, int64_t group) {
 // tokens that a wave loads: 4, 8 or 16
 constexpr int token_class(int64_t B) { return B <= 4 ? 4 : B <= 8 ? 8 : 16; }
 
-// Tiles of a wave of the matrix-vector product.  Two tiles share the tokens' way through LDS, which counts for 16 tokens from 8192 rows on (14336 x
-// 4096, B = 16: 10.2 us with two, 12.3 with one; 4096 x 14336: 14.4 and 11.8), for up to 4 where memory is kept busy by half as many
-// waves (73728 x 4608, B = 1, r = 4: 34.9 and 37.0 us; 28672 x 4096: 13.5 and 13.0), at two bits, which are bound by the vector unit, earlier
-// (28672 x 4096: 12.9 and 13.5).  Groups of 32 at four bits leave no registers for it (73728 x 4608: 57 and 51 us).
+// Tiles of a wave of the matrix-vector product.  Two tiles share the tokens' way through LDS and halve the workgroups.  us with one and two, K = 4096
+// (r = 4 and up to 4 tokens: 4608), groups of 128 (r = 8: of 64):
+//   16 tokens, r = 4   8192 rows 8.2-8.8, 7.0    12288 10.2, 10.1    28672 19.0, 16.5   (K = 14336, groups of 32, 4096 rows: 11.8, 14.4)
+//              r = 2   8192 rows 8.0, 7.7        12288 10.6, 10.6    28672 21.1, 19.1   (4096: 6.6, 7.5)
+//              r = 8   8192 rows 11.1, 10.0      12288 15.2, 14.3    28672 36.5, 33.1   (4096: 7.5, 7.7)
+//    8 tokens, r = 4   8192 rows 7.2, 6.5        12288 9.1, 8.8      28672 15.6, 14.3;   r = 2   8192 rows 6.9, 6.9   28672 16.2, 15.3
+//              r = 8   8192 rows 10.9, 10.0      28672 31.2, 29.3
+//     1 token, r = 4   28672 rows 15.3, 19.0     40960 22.4, 23.7    57344 29.8, 28.5    65536 33.3, 32.6    73728 36.0, 35.2
+//              r = 2   12288 rows 7.9, 8.9       16384 9.5, 9.2      20480 11.0, 11.1    28672 13.8, 13.7    73728 31.6, 27.6
+//              r = 8   8192 rows 10.5, 9.7       16384 16.8, 15.6    28672 28.9, 31.4    73728 64.3, 63.3    (16384, K = 14336: 47.3, 49.3)
+//    4 tokens, r = 4   57344 rows 32.7, 30.1     73728 41.6, 37.6
+// so at eight bits it is as often a few percent too many as too few up to 4 tokens.  Groups of 32 at four bits leave no registers for it there
+// (73728 x 4608: 51 us, 57).
 constexpr bool gemv_two_tiles_fit(int r, int chunk, int tokens) { return tokens > 4 || r != 4 || chunk != 32; }
 constexpr int gemv_tiles(int r, int chunk, int64_t B, int64_t N) {
     return gemv_two_tiles_fit(r, chunk, token_class(B)) && N >= (B > 4 ? 8192 : r == 4 ? 65536 : 16384) ? 2 : 1;
